@@ -367,6 +367,124 @@ prcr_status prcr_decode_attention_static(const prcr_rope *rope, const prcr_cache
                                          float scale, float *out, int32_t *err_flag,
                                          hipStream_t stream);
 
+/*
+ * Operators on several new tokens per sequence.  Their query rows are packed: q is
+ * [total_q][n_q_heads][head_dim], raw (pre-rotary), and sequence b's rows are
+ * q_off[b] .. q_off[b+1] - 1 (int32 [batch+1], 0 <= q_off[b] <= q_off[b+1] <= total_q), or, with
+ * q_len (int32 [batch]; NULL: all of them), only the first q_len[b] of those: a padded
+ * [batch][s_max] array of rows is q_off[b] = b s_max with q_len.  q_pos is int32 [total_q][3],
+ * the rows' (t, h, w) positions.  The rows are the sequence's newest tokens, already in
+ * the cache: with n_b of them, row i stands at slot cache_len[b] - n_b + i and sees the slots up
+ * to that one.  A whole prompt is n_b = cache_len[b]; a decoded token n_b = 1.
+ *
+ * Queries are rotated as prcr_prefill_capture rotates keys: in double precision, rounded
+ * once to dtype.  Any number of query heads per KV head.  The capacity per sequence
+ * (s_max, or max_blocks * block_size) and total_q * n_q_heads are at most 2^30, else
+ * PRCR_ERR_SHAPE; head_dim 64 or 128 and the axis maps of prcr_rebind_inject.  A cache_len beyond
+ * the capacity is clamped with PRCR_DERR_CAPACITY; a sequence with malformed offsets or
+ * q_len has no rows (PRCR_DERR_OFFSETS); a block-table entry outside the pool skips its keys
+ * (PRCR_DERR_BLOCK).  Outputs and workspace must not share memory with an input or
+ * with each other (PRCR_ERR_ALIAS).  total_q = 0 is allowed.
+ */
+
+/*
+ * prcr_chunk_attention - causal attention of the rows over one layer of the cache:
+ *   s_j = scale q' . k_j,  lse = log sum_j exp(s_j),  out = sum_j exp(s_j - lse) v_j
+ * over the slots j that the row sees, q' the rotated row.
+ *
+ *   out           [total_q][n_q_heads][head_dim], dtype, 16-byte aligned
+ *   lse           float32 [total_q][n_q_heads], or NULL
+ *   workspace     prcr_chunk_workspace_size() bytes, 16-byte aligned
+ * Scores, the softmax and the sums are float32; bfloat16 weights are rounded to
+ * bfloat16 for the product with the values (their sum is taken before that), and out is rounded once.  A row
+ * that sees no slot gets out = 0 and lse = -infinity.  Values and keys at slots that a row
+ * does not see have no influence on it, whatever they are; a NaN at one that it sees makes it NaN.
+ * Rows of no sequence (padding, rows behind the last sequence) are left as they were.
+ */
+prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,
+                                 prcr_dtype dtype, int32_t batch, int32_t n_layers,
+                                 int32_t n_kv_heads, int32_t layer, const void *q,
+                                 int32_t n_q_heads, const int32_t *q_off,
+                                 const int32_t *q_len, int32_t total_q,
+                                 const int32_t *q_pos, const int32_t *cache_len,
+                                 float scale, void *out, float *lse, void *workspace,
+                                 size_t workspace_bytes, int32_t *err_flag,
+                                 hipStream_t stream);
+
+/* Workspace bytes prcr_chunk_attention needs for this cache and shape (host). */
+prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, prcr_dtype dtype,
+                                      int32_t batch, int32_t total_q, int32_t n_q_heads,
+                                      int32_t n_kv_heads, int32_t head_dim, size_t *bytes);
+
+/*
+ * prcr_key_weights - the attention weight that each cached key gets from the rows:
+ *   weights[b][h][j] = sum of exp(s_j - lse) over the rows of sequence b that see slot j
+ *                      and the query heads of KV head h
+ * with s_j and lse as prcr_chunk_attention has them for the same rows, layer and scale.
+ *
+ *   lse           float32 [total_q][n_q_heads], from prcr_chunk_attention
+ *   window        only the last `window` rows of each sequence count; 0: all
+ *   weights       float32 [batch][n_kv_heads][capacity].  accumulate != 0: added to what is there
+ *                 (over layers, or decoded tokens); slots from cache_len[b] on are left as they
+ *                 were.  accumulate == 0: every slot is written, 0 from cache_len[b] on.
+ *   workspace     prcr_key_weights_workspace_size() bytes, 16-byte aligned
+ * Rows are summed 16 at a time in float32 and those sums in double, in an order that depends
+ * on the lengths alone; the result is rounded to float32 and added.  A row with lse =
+ * -infinity sees nothing and gives nothing.
+ */
+prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache,
+                             prcr_dtype dtype, int32_t batch, int32_t n_layers,
+                             int32_t n_kv_heads, int32_t layer, const void *q,
+                             int32_t n_q_heads, const int32_t *q_off, const int32_t *q_len,
+                             int32_t total_q, const int32_t *q_pos,
+                             const int32_t *cache_len, const float *lse, int32_t window,
+                             float scale, int32_t accumulate, float *weights,
+                             void *workspace, size_t workspace_bytes, int32_t *err_flag,
+                             hipStream_t stream);
+
+/* Workspace bytes prcr_key_weights needs (host). */
+prcr_status prcr_key_weights_workspace_size(prcr_dtype dtype, int32_t total_q,
+                                            int32_t n_q_heads, int32_t head_dim,
+                                            size_t *bytes);
+
+/*
+ * prcr_evict - cuts every sequence of more than `budget` slots back to `budget`, by the
+ * weight its keys received, and moves what is kept to the front of the cache in all layers.
+ *
+ * Of a longer sequence the first keep_first and the last keep_last slots are kept, and of
+ * the others the budget - keep_first - keep_last highest by score; the score of a slot is
+ * the sum of its heads' weights, in double, rounded to float32.  Equal scores: the lower slots; a
+ * NaN ranks below every number.  Kept slots keep their order: kept[b][i] moves to slot i (its
+ * key was rotated at the token's own position, which stays).
+ *
+ *   weights        float32 [batch][n_kv_heads][capacity], as prcr_key_weights fills them
+ *   budget         >= 1;  keep_first, keep_last >= 0, their sum at most budget
+ *   new_cache_len  out int32 [batch]: min(cache_len[b], budget); may be cache_len itself
+ *   kept           out int32 [batch][budget]: the kept slots, ascending, then -1
+ *   new_weights    out, as weights, or NULL: the kept slots' weights at their new slots, 0 from
+ *                  new_cache_len[b] on
+ *   mem            NULL, or a memory of this batch whose values live in the cache (mem->v ==
+ *                  NULL): mem->v_slot is renamed in place, -1 where the slot was not kept
+ *                  (a revisit of that token then raises PRCR_DERR_INDEX and skips it).  Only
+ *                  v, v_slot, batch and max_visual of it are read.  Such memories must
+ *                  be given: their slots are wrong after the call otherwise.
+ *   workspace      prcr_evict_workspace_size() bytes
+ * Rows of slots from new_cache_len[b] on are left as they are.  Paged: the block table stays; blocks
+ * past the new length are the caller's to reuse, and a sequence's blocks must not be
+ * another one's too.  A block-table entry outside the pool skips its rows (PRCR_DERR_BLOCK).
+ * No output may share memory with another array (PRCR_ERR_ALIAS), but new_cache_len be cache_len.
+ */
+prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
+                       int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                       const int32_t *cache_len, const float *weights, int32_t budget,
+                       int32_t keep_first, int32_t keep_last, int32_t *new_cache_len,
+                       int32_t *kept, float *new_weights, const prcr_mem *mem,
+                       void *workspace, size_t workspace_bytes, int32_t *err_flag,
+                       hipStream_t stream);
+
+/* Workspace bytes prcr_evict needs (host). */
+prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch, size_t *bytes);
+
 /* Host helpers (no GPU work). */
 
 /* Static description of a status code (host). */

@@ -109,6 +109,28 @@ def lib() -> ctypes.CDLL:
     L.prcr_revisit.argtypes = [POINTER(CRope), POINTER(CMem), c_void_p, c_void_p, c_int32, c_void_p,
                                c_int, c_int32, POINTER(CCache), c_void_p, c_void_p, c_void_p,
                                c_void_p, c_void_p, c_void_p, c_void_p]
+    L.prcr_chunk_workspace_size.restype = c_int
+    L.prcr_chunk_workspace_size.argtypes = [POINTER(CCache), c_int, c_int32, c_int32, c_int32, c_int32,
+                                            c_int32, POINTER(ctypes.c_size_t)]
+    L.prcr_chunk_attention.restype = c_int
+    L.prcr_chunk_attention.argtypes = [POINTER(CRope), POINTER(CCache), c_int, c_int32, c_int32,
+                                       c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                       c_int32, c_void_p, c_void_p, ctypes.c_float, c_void_p,
+                                       c_void_p, c_void_p, ctypes.c_size_t, c_void_p, c_void_p]
+    L.prcr_key_weights_workspace_size.restype = c_int
+    L.prcr_key_weights_workspace_size.argtypes = [c_int, c_int32, c_int32, c_int32,
+                                                  POINTER(ctypes.c_size_t)]
+    L.prcr_key_weights.restype = c_int
+    L.prcr_key_weights.argtypes = [POINTER(CRope), POINTER(CCache), c_int, c_int32, c_int32, c_int32,
+                                   c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_int32,
+                                   c_void_p, c_void_p, c_void_p, c_int32, ctypes.c_float, c_int32,
+                                   c_void_p, c_void_p, ctypes.c_size_t, c_void_p, c_void_p]
+    L.prcr_evict_workspace_size.restype = c_int
+    L.prcr_evict_workspace_size.argtypes = [POINTER(CCache), c_int32, POINTER(ctypes.c_size_t)]
+    L.prcr_evict.restype = c_int
+    L.prcr_evict.argtypes = [POINTER(CCache), c_int, c_int32, c_int32, c_int32, c_int32, c_void_p,
+                             c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
+                             POINTER(CMem), c_void_p, ctypes.c_size_t, c_void_p, c_void_p]
     _LIB = L
     return L
 
@@ -629,3 +651,183 @@ def decode_attention_static(rope: Rope, cache: Cache, layer: int, q, q_pos, cach
                                             _stream(stream, cache.device))
     _check("prcr_decode_attention_static", st)
     return out
+
+
+def _capacity(cache: Cache) -> int:
+    """Slots a sequence of a cache has."""
+    return cache.block_table.shape[1] * cache.k.shape[2] if cache.paged else cache.k.shape[3]
+
+
+def _batch(cache: Cache) -> int:
+    return cache.block_table.shape[0] if cache.paged else cache.k.shape[0]
+
+
+def _size_t(fn: str, *args) -> int:
+    out = ctypes.c_size_t(0)
+    _check(fn, getattr(lib(), fn)(*args, ctypes.byref(out)))
+    return int(out.value)
+
+
+def _workspace(workspace, need, device, stream):
+    torch = _torch()
+    if workspace is None:
+        return _new(((max(need, 4) + 3) // 4,), torch.float32, device, stream, given=False)
+    _need(workspace, "workspace", None, None, device)
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace needs {need} bytes")
+    return workspace
+
+
+def _query_rows(cache: Cache, q, q_off, q_pos, cache_len, q_len):
+    """Checks of the packed query rows; (batch, rows, query heads)."""
+    torch = _torch()
+    NL, H, D = _cache_dims(cache)
+    _need(q, "q", cache.k.dtype, 3, cache.device)
+    T, Hq = q.shape[0], q.shape[1]
+    if q.shape[2] != D:
+        raise ValueError("q head_dim differs from the cache's")
+    B = _batch(cache)
+    _need(q_off, "q_off", torch.int32, 1, cache.device)
+    _shape(q_off, "q_off", (B + 1,))
+    if q_len is not None:
+        _need(q_len, "q_len", torch.int32, 1, cache.device)
+        _shape(q_len, "q_len", (B,))
+    _need(q_pos, "q_pos", torch.int32, 2, cache.device)
+    _shape(q_pos, "q_pos", (T, 3))
+    _need(cache_len, "cache_len", torch.int32, 1, cache.device)
+    _shape(cache_len, "cache_len", (B,))
+    return B, T, Hq
+
+
+def chunk_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int) -> int:
+    """Bytes of workspace prcr_chunk_attention needs (prcr_chunk_workspace_size)."""
+    NL, H, D = _cache_dims(cache)
+    return _size_t("prcr_chunk_workspace_size", ctypes.byref(cache.to_c()), _dtype_code(cache.k),
+                   _batch(cache), int(total_q), int(n_q_heads), int(H), int(D))
+
+
+def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len, q_len=None,
+                    scale=None, out=None, lse=None, workspace=None, err=None, stream=None):
+    """Causal attention of several new tokens per sequence, or of whole prompts, over one
+    layer of the cache that already holds them (prcr_chunk_attention).  q [T, Hq, D] raw
+    queries, packed: sequence b's rows are q_off[b] .. q_off[b + 1] - 1 (q_off [B + 1]), or the
+    first q_len[b] of those; q_pos [T, 3] their (t, h, w) positions.  Returns (out [T, Hq, D] in
+    the cache's type, lse [T, Hq] float32); rows of no sequence are not written."""
+    done = (_NATIVE or _native()).chunk_attention(rope, cache, layer, q, q_off, q_pos, cache_len, q_len,
+                                                  scale, out, lse, workspace, err, stream)
+    if done is not None:
+        return _done("prcr_chunk_attention", done)
+    torch = _torch()
+    NL, H, D = _cache_dims(cache)
+    B, T, Hq = _query_rows(cache, q, q_off, q_pos, cache_len, q_len)
+    if out is None:
+        out = _new((T, Hq, D), cache.k.dtype, cache.device, stream)
+    if lse is None:
+        lse = _new((T, Hq), torch.float32, cache.device, stream)
+    _need(out, "out", cache.k.dtype, 3, cache.device)
+    _shape(out, "out", (T, Hq, D))
+    _need(lse, "lse", torch.float32, 2, cache.device)
+    _shape(lse, "lse", (T, Hq))
+    workspace = _workspace(workspace, chunk_workspace_bytes(cache, T, Hq), cache.device, stream)
+    _err(err, cache.device)
+    sc = float(D) ** -0.5 if scale is None else float(scale)
+    st = lib().prcr_chunk_attention(
+        ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H),
+        int(layer), _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len), sc,
+        _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err),
+        _stream(stream, cache.device))
+    _check("prcr_chunk_attention", st)
+    return out, lse
+
+
+def key_weights_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int) -> int:
+    """Bytes of workspace prcr_key_weights needs (prcr_key_weights_workspace_size)."""
+    return _size_t("prcr_key_weights_workspace_size", _dtype_code(cache.k), int(total_q), int(n_q_heads),
+                   int(_cache_dims(cache)[2]))
+
+
+def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len, lse, q_len=None,
+                window=None, scale=None, weights=None, accumulate: bool = False, workspace=None,
+                err=None, stream=None):
+    """The attention weight that each cached key of one layer gets from the rows of
+    chunk_attention (prcr_key_weights), whose lse it takes; window: from the last so many rows of
+    each sequence only.  Returns weights [B, H, capacity] float32, added to with accumulate."""
+    done = (_NATIVE or _native()).key_weights(rope, cache, layer, q, q_off, q_pos, cache_len, lse, q_len,
+                                              window, scale, weights, accumulate, workspace, err, stream)
+    if done is not None:
+        return _done("prcr_key_weights", done)
+    torch = _torch()
+    NL, H, D = _cache_dims(cache)
+    B, T, Hq = _query_rows(cache, q, q_off, q_pos, cache_len, q_len)
+    _need(lse, "lse", torch.float32, 2, cache.device)
+    _shape(lse, "lse", (T, Hq))
+    if window is not None and int(window) < 1:
+        raise ValueError("window must be at least 1 (None: all rows)")
+    if weights is None:
+        if accumulate:
+            raise ValueError("accumulate needs the weights to add to")
+        weights = _new((B, H, _capacity(cache)), torch.float32, cache.device, stream)
+    _need(weights, "weights", torch.float32, 3, cache.device)
+    _shape(weights, "weights", (B, H, _capacity(cache)))
+    workspace = _workspace(workspace, key_weights_workspace_bytes(cache, T, Hq), cache.device, stream)
+    _err(err, cache.device)
+    sc = float(D) ** -0.5 if scale is None else float(scale)
+    st = lib().prcr_key_weights(
+        ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H),
+        int(layer), _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len),
+        _ptr(lse), 0 if window is None else int(window), sc, int(bool(accumulate)), _ptr(weights),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err),
+        _stream(stream, cache.device))
+    _check("prcr_key_weights", st)
+    return weights
+
+
+def evict_workspace_bytes(cache: Cache) -> int:
+    """Bytes of workspace prcr_evict needs (prcr_evict_workspace_size)."""
+    return _size_t("prcr_evict_workspace_size", ctypes.byref(cache.to_c()), _batch(cache))
+
+
+def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, keep_last: int = 0, mem=None,
+          new_cache_len=None, kept=None, new_weights=None, workspace=None, err=None, stream=None):
+    """Cuts every sequence of more than `budget` slots back to `budget`: its first keep_first and
+    last keep_last ones and the highest by weight between them, moved in order to the front of the
+    cache in every layer (prcr_evict).  A memory whose values live in this cache (key-only) must
+    be given as mem: its slots are renamed.  Returns (new_cache_len [B] int32, kept [B, budget]
+    int32 (-1 behind the kept ones), new_weights [B, H, capacity])."""
+    done = (_NATIVE or _native()).evict(cache, cache_len, weights, budget, keep_first, keep_last, mem,
+                                        new_cache_len, kept, new_weights, workspace, err, stream)
+    if done is not None:
+        return _done("prcr_evict", done)
+    torch = _torch()
+    NL, H, D = _cache_dims(cache)
+    B, cap = _batch(cache), _capacity(cache)
+    budget = int(budget)
+    _need(cache_len, "cache_len", torch.int32, 1, cache.device)
+    _shape(cache_len, "cache_len", (B,))
+    _need(weights, "weights", torch.float32, 3, cache.device)
+    _shape(weights, "weights", (B, H, cap))
+    if budget < 1 or keep_first < 0 or keep_last < 0 or keep_first + keep_last > budget:
+        raise ValueError("budget must be at least 1 and hold keep_first + keep_last slots")
+    if mem is not None and mem.device != cache.device:
+        raise ValueError(f"mem is on {mem.device}, expected {cache.device}")
+    if new_cache_len is None:
+        new_cache_len = _new((B,), torch.int32, cache.device, stream)
+    if kept is None:
+        kept = _new((B, budget), torch.int32, cache.device, stream)
+    if new_weights is None:
+        new_weights = _new((B, H, cap), torch.float32, cache.device, stream)
+    _need(new_cache_len, "new_cache_len", torch.int32, 1, cache.device)
+    _shape(new_cache_len, "new_cache_len", (B,))
+    _need(kept, "kept", torch.int32, 2, cache.device)
+    _shape(kept, "kept", (B, budget))
+    _need(new_weights, "new_weights", torch.float32, 3, cache.device)
+    _shape(new_weights, "new_weights", (B, H, cap))
+    workspace = _workspace(workspace, evict_workspace_bytes(cache), cache.device, stream)
+    _err(err, cache.device)
+    st = lib().prcr_evict(
+        ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H), int(D), _ptr(cache_len),
+        _ptr(weights), budget, int(keep_first), int(keep_last), _ptr(new_cache_len), _ptr(kept),
+        _ptr(new_weights), None if mem is None else ctypes.byref(mem.to_c()), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
+    _check("prcr_evict", st)
+    return new_cache_len, kept, new_weights

@@ -26,7 +26,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 # not part of the PRCR path or its ABI.
 COPYREF_SOURCES = ["copyref.hip"]
 COPYREF_OUT = os.path.join(PKG, "libprcr_copyref.so")
-SOURCES = ["api.cpp", "axis_map.cpp", "decode.hip", "decode_static.hip", "prefill.hip", "reassign.hip", "rebind.hip", "store_raw.hip"]
+SOURCES = ["api.cpp", "attend_api.cpp", "axis_map.cpp", "chunk.hip", "decode.hip", "decode_static.hip", "evict.hip",
+           "key_weights.hip", "prefill.hip", "reassign.hip", "rebind.hip", "rotate_rows.hip", "store_raw.hip"]
 
 # The binding's native module: C++ against torch's and Python's headers.
 NATIVE_SOURCE = "native_calls.cpp"

@@ -1,0 +1,130 @@
+// Shared by the operators on several tokens per sequence: chunk attention, the keys'
+// weights and eviction.  Parameter blocks, launchers, and the device side of the packed
+// query rows and of a cache row's address.
+#pragma once
+
+#include <cfloat>
+#include <cstdint>
+
+#include <hip/hip_runtime.h>
+
+#include "prcr_internal.h"
+
+namespace prcr {
+
+// Packed query rows and the cache they look at.  Query row t of total_q is a token; a
+// sequence's rows are q_off[b] .. q_off[b + 1] - 1, or the first q_len[b] of them.
+struct AttendParams {
+  const void *q;                  // [total_q][n_q_heads][head_dim], as given
+  void *rotated;                  // the same, rotated (workspace)
+  const int32_t *q_off;           // [batch + 1]
+  const int32_t *q_len;           // [batch] or null
+  const int32_t *q_pos;           // [total_q][3]
+  const int32_t *cache_len;       // [batch]
+  const void *cache_k;
+  const void *cache_v;
+  const int32_t *block_table;
+  void *out;                      // chunk attention: [total_q][n_q_heads][head_dim]
+  float *lse;                     // [total_q][n_q_heads]: out (or null), or the weights' input
+  float *part;                    // chunk attention: [total_q][n_q_heads][n_split][head_dim + 2]
+  float *weights;                 // weights: [batch][n_kv_heads][capacity]
+  int32_t *err;
+  int32_t total_q, batch, n_layers, n_kv_heads, n_q_heads, group, layer;
+  int32_t s_max, block_size, max_blocks, n_blocks;
+  int32_t block_shift;            // log2(block_size) if a power of two, else -1
+  int32_t capacity;               // slots per sequence: s_max, or max_blocks * block_size
+  int32_t n_slots, n_split;       // chunk attention: row tiles there is room for, key splits (launcher)
+  int32_t window;                 // weights: the last rows of each sequence that count (0: all)
+  int32_t accumulate;
+  float scale;                    // |scale|; a negative one turns the rotated queries' sign
+  float scale2;                   // |scale| log2(e)
+  int32_t negate;
+  Divisor by_group, by_heads, by_split;
+  int8_t axis[kMaxPairs];
+  double inv_freq[kMaxPairs];
+};
+
+struct EvictParams {
+  const int32_t *cache_len;
+  const float *weights;           // [batch][n_kv_heads][capacity]
+  void *cache_k;
+  void *cache_v;
+  const int32_t *block_table;
+  int32_t *new_len;               // [batch]
+  int32_t *kept;                  // [batch][budget]
+  float *new_weights;             // [batch][n_kv_heads][capacity] or null
+  int32_t *v_slot;                // [batch][max_visual] of a key-only memory, or null
+  float *score;                   // workspace [batch][capacity]
+  int32_t *err;
+  int32_t batch, n_layers, n_kv_heads, row_bytes;
+  int32_t s_max, block_size, max_blocks, n_blocks, capacity;
+  int32_t budget, keep_first, keep_last, max_visual;
+};
+
+// What a call of chunk attention needs besides its arguments: how its rows and keys are
+// divided, and the bytes of its workspace (rotated queries, then partial results).
+struct ChunkPlan {
+  int32_t waves;                  // per workgroup: a tile is 32 rows a wave
+  int32_t n_slots, n_split;
+  size_t rotated_bytes, bytes;
+};
+ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
+                     int32_t head_dim, prcr_dtype dtype);
+
+hipError_t launch_rotate(const AttendParams &p, prcr_dtype dtype, int head_dim, hipStream_t stream);
+hipError_t launch_chunk(const AttendParams &p, const ChunkPlan &plan, prcr_dtype dtype, int head_dim, bool paged,
+                        hipStream_t stream);
+hipError_t launch_key_weights(const AttendParams &p, prcr_dtype dtype, int head_dim, bool paged, hipStream_t stream);
+hipError_t launch_evict(const EvictParams &p, bool paged, hipStream_t stream);
+
+#ifdef __HIPCC__
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The rows of sequence b: its first row and their count (0 where the offsets are malformed),
+// and whether they are.
+struct Rows {
+  int32_t start, n;
+  bool bad;
+};
+__device__ __forceinline__ Rows rows_of(const AttendParams &p, int b) {
+  const int32_t s = p.q_off[b], e = p.q_off[b + 1];
+  Rows r{s, e - s, s < 0 || e < s || e > p.total_q};
+  if (p.q_len != nullptr && !r.bad) {
+    const int32_t n = p.q_len[b];
+    r.bad = n < 0 || n > r.n;
+    r.n = n;
+  }
+  if (r.bad) r.n = 0;
+  return r;
+}
+
+__device__ __forceinline__ int32_t clamp_length(int32_t len, int32_t capacity) { return min(max(len, 0), capacity); }
+
+// The larger of each lane's value and that of the lane 32 away.
+__device__ __forceinline__ float half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {   // to nearest, ties to even
+  const f32x2 x = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
+}  // namespace
+#endif
+
+}  // namespace prcr

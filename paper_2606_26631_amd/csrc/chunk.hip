@@ -1,0 +1,490 @@
+// Attention of several new tokens per sequence over the active cache: with row i of
+// sequence b's n_b rows at slot p = cache_len[b] - n_b + i,
+//   out = sum over slots j <= p of exp(s_j - lse) v_j,  s_j = scale q' . k_j,
+//   lse = log sum over slots j <= p of exp(s_j),
+// q' the rotated query.  A whole prompt is the case n_b = cache_len[b].
+//
+// A workgroup takes a tile of rows of one sequence and KV head, 32 rows a wave; the rows of a
+// KV head are its tokens' query heads, token by token, so that a tile reads the cache
+// once for all heads of the group.  Tiles of keys and values go through LDS, two of them,
+// the next one's loads in flight while the present one is used.  The wave forms the scores
+// transposed, K (32 keys) x Q^T (32 rows): a lane then holds scores of one row only (that
+// of its product column), the running maximum and sum of the softmax are one register
+// each, and the weights are, in the registers where they arise, the operand of the value
+// product V^T x P^T, whose contraction may take the keys in any order.
+#include <algorithm>
+#include <type_traits>
+
+#include "attend.h"
+#include "rotary.h"
+
+namespace prcr {
+namespace {
+
+// 16 bytes per lane from memory to LDS: lane l's go to `to` + 16 l.
+__device__ __forceinline__ void load_to_lds(const char *from, char *to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                   (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// The sequence that tile slot `slot` belongs to: sequence b has the slots from
+// floor(q_off[b] G / M) + b on, enough of them for its rows' tiles of M.
+template <int M>
+__device__ __forceinline__ int32_t first_slot(const AttendParams &p, int b) {
+  const uint32_t off = static_cast<uint32_t>(min(max(p.q_off[b], 0), p.total_q));
+  return static_cast<int32_t>(off * static_cast<uint32_t>(p.group) / M) + b;
+}
+template <int M>
+__device__ __forceinline__ int sequence_of_slot(const AttendParams &p, int lane, int slot) {
+  int lo = 0, n = p.batch;                   // among sequences lo .. lo + n - 1, the last that starts by `slot`
+  while (n > kWave) {
+    const int step = (n + kWave - 1) / kWave;
+    const int b = lo + lane * step;
+    const bool ok = lane * step < n && first_slot<M>(p, b) <= slot;
+    const int k = max(__popcll(__ballot(ok)) - 1, 0) * step;
+    lo += k;
+    n = min(step, n - k);
+  }
+  const bool ok = lane < n && first_slot<M>(p, lo + lane) <= slot;
+  return __builtin_amdgcn_readfirstlane(lo + max(__popcll(__ballot(ok)) - 1, 0));
+}
+
+// What a tile of the cache's rows in LDS looks like.  A row's 16-byte chunks are permuted
+// by the row's number, so that the lanes of one read fall on different banks: key rows, which
+// are read 32 rows at a time at one chunk, over the whole row; value rows, which are read 4
+// (bf16) neighbouring rows at a time at 4 chunks, by steps of 4 chunks.
+template <typename T, int D>
+struct TileOf {
+  static constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int kRowBytes = D * static_cast<int>(sizeof(T));
+  static constexpr int kChunks = kRowBytes / 16;
+  static constexpr int kBytes = kKeys * kRowBytes;
+  static constexpr int kRowsPerLoad = kWave / kChunks;
+  static constexpr int kLoads = kKeys / kRowsPerLoad;    // wave loads of a tile
+  __device__ static constexpr int key_swizzle(int row) { return row & (kChunks - 1); }
+  __device__ static constexpr int value_swizzle(int row) {
+    if constexpr (sizeof(T) == 4) return 0;
+    return kChunks == 16 ? (row & 3) << 2 : (row >> 1 & 1) << 2;
+  }
+};
+
+template <typename T, int D, bool kPaged, int kWaves>
+__global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendParams p) {
+  using Tile = TileOf<T, D>;
+  constexpr bool kHalf = sizeof(T) == 2;     // bf16
+  constexpr int M = 32 * kWaves;
+  constexpr int KT = Tile::kKeys, kRowBytes = Tile::kRowBytes;
+  constexpr int KB = KT / 32;                // key blocks of a tile
+  constexpr int DT = D / 32;                 // feature blocks
+  constexpr int kMine = Tile::kLoads / kWaves;   // loads of each operand per wave and tile
+  __shared__ __align__(1024) char s_kv[2][2][Tile::kBytes];
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int l32 = lane & 31, half = lane / 32;
+  uint32_t id = blockIdx.x;
+  const uint32_t by_head = p.by_heads.divide(id);
+  const int kvh = static_cast<int>(id - by_head * static_cast<uint32_t>(p.n_kv_heads));
+  const uint32_t by_split = p.by_split.divide(by_head);
+  const int split = static_cast<int>(by_head - by_split * static_cast<uint32_t>(p.n_split));
+  const int slot = p.n_slots - 1 - static_cast<int>(by_split);   // a prompt's last tiles see the most keys: first
+  const int b = sequence_of_slot<M>(p, lane, slot);
+  const Rows rows = rows_of(p, b);
+  const int32_t len = clamp_length(p.cache_len[b], p.capacity);
+  const int G = p.group;
+  const int n_rows = rows.n * G;
+  const int r0 = (slot - first_slot<M>(p, b)) * M;
+  if (r0 < 0 || r0 >= n_rows) return;
+
+  const int first = len - rows.n;            // slot of the sequence's first row
+  auto token_of = [&](int r) -> int { return static_cast<int>(p.by_group.divide(static_cast<uint32_t>(r))); };
+  const int kend = first + token_of(min(r0 + M, n_rows) - 1) + 1;   // (at most len)
+  const int n_tiles = max((kend + KT - 1) / KT, 0);
+  const int per = (n_tiles + p.n_split - 1) / p.n_split;
+  const int t0 = min(split * per, n_tiles), t1 = min(t0 + per, n_tiles);
+
+  // The lane's row, and the last slots that it, the wave's first row and its last one see.
+  const int wr0 = r0 + wave * 32;
+  const bool active = wr0 < n_rows;
+  const int r = min(wr0 + l32, n_rows - 1);
+  const int token = token_of(r);
+  const int64_t row = (static_cast<int64_t>(rows.start) + token) * p.n_q_heads + kvh * G + (r - token * G);
+  const int limit = first + token;
+  const int wmin = __builtin_amdgcn_readfirstlane(limit);
+  const int wmax = __builtin_amdgcn_readlane(limit, 31);
+
+  // Query operand.  bf16: of product kk, elements 16 kk + 8 half + 0..7.  float32: the
+  // lane's half of the row, in order.
+  constexpr int kQ = kHalf ? D / 16 : D / 8;   // 16-byte chunks
+  u32x4 q[kQ];
+  {
+    const char *at = static_cast<const char *>(p.rotated) + row * kRowBytes;
+#pragma unroll
+    for (int i = 0; i < kQ; ++i)
+      q[i] = *reinterpret_cast<const u32x4 *>(at + (kHalf ? 2 * i + half : half * kQ + i) * 16);
+  }
+
+  // Rows of a tile: every load is issued for a row that exists; rows past the sequence's last
+  // one, or in a block outside the pool, are left out by the mask.
+  const int64_t pool = static_cast<int64_t>(p.layer) * p.n_blocks * p.block_size;
+  const int64_t base = (kPaged ? pool * p.n_kv_heads + kvh
+                               : ((static_cast<int64_t>(b) * p.n_layers + p.layer) * p.n_kv_heads + kvh) * p.s_max) *
+                       kRowBytes;
+  const char *const base_k = static_cast<const char *>(p.cache_k) + base;
+  const char *const base_v = static_cast<const char *>(p.cache_v) + base;
+  const uint32_t row_step = kPaged ? static_cast<uint32_t>(p.n_kv_heads) * kRowBytes : kRowBytes;
+  const int32_t *const table = kPaged ? p.block_table + static_cast<int64_t>(b) * p.max_blocks : nullptr;
+  int bad_block = 0;
+  // Slot in the layer's pool of key `lane % KT` of tile t; -1 in a block outside it.
+  // (A pool's slots are at least 128 bytes each: below 2^32 of them.)
+  auto entry_of = [&](int t, int32_t *off) -> int32_t {
+    const int j = min(t * KT + lane % KT, len - 1);
+    const int lb = p.block_shift >= 0 ? j >> p.block_shift : j / p.block_size;
+    *off = j - lb * p.block_size;
+    return table[lb];
+  };
+  int32_t entry = 0, entry_off = 0;
+  const int in_load = lane / Tile::kChunks, chunk = lane % Tile::kChunks;
+  auto load_tile = [&](int t, char (*to)[Tile::kBytes]) -> uint64_t {
+    uint64_t live = ~uint64_t{0};
+    uint32_t pool_slot = 0;
+    if constexpr (kPaged) {
+      const bool ok = entry >= 0 && entry < p.n_blocks;
+      live = __ballot(ok);
+      bad_block |= !ok && t * KT + lane % KT < len;
+      pool_slot = ok ? static_cast<uint32_t>(entry) * static_cast<uint32_t>(p.block_size) +
+                           static_cast<uint32_t>(entry_off) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int load = i * kWaves + wave;
+      const int at = load * Tile::kRowsPerLoad + in_load;        // the lane's row of the tile
+      int64_t from;
+      if constexpr (kPaged)
+        from = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(pool_slot), at))) *
+                                    row_step);
+      else
+        from = static_cast<int64_t>(min(t * KT + at, len - 1)) * row_step;
+      load_to_lds(base_k + from + (chunk ^ Tile::key_swizzle(at)) * 16, to[0] + load * 1024);
+      load_to_lds(base_v + from + (chunk ^ Tile::value_swizzle(at)) * 16, to[1] + load * 1024);
+    }
+    return live;
+  };
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  float m = -FLT_MAX, l = 0.f;               // running maximum (base 2), the lane's own keys' sum
+
+  uint64_t live = ~uint64_t{0}, live_next = ~uint64_t{0};
+  if (t0 < t1) {
+    if constexpr (kPaged) entry = entry_of(t0, &entry_off);
+    live_next = load_tile(t0, s_kv[t0 & 1]);
+    if constexpr (kPaged) entry = entry_of(min(t0 + 1, t1 - 1), &entry_off);
+  }
+  for (int t = t0; t < t1; ++t) {
+    // The tile's loads have arrived, in every wave, and every wave is done with the other buffer.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    live = live_next;
+    if (t + 1 < t1) {
+      live_next = load_tile(t + 1, s_kv[(t + 1) & 1]);
+      if constexpr (kPaged) entry = entry_of(min(t + 2, t1 - 1), &entry_off);
+    }
+    const int k0 = t * KT;
+    if (!active || k0 > wmax) continue;
+    const char *const kt = s_kv[t & 1][0];
+    const char *const vt = s_kv[t & 1][1];
+
+    // Scores: lane's keys 32 kb + 8 (i / 4) + 4 half + i % 4 of row l32.
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+      const char *const krow = kt + (32 * kb + l32) * kRowBytes;
+      const int sw = Tile::key_swizzle(l32);   // (32 kb changes nothing in it)
+#pragma unroll
+      for (int i = 0; i < kQ; ++i) {
+        if constexpr (kHalf) {
+          const u32x4 k = *reinterpret_cast<const u32x4 *>(krow + ((2 * i + half) ^ sw) * 16);
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
+                                                          __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
+        } else {
+          const f32x4 k = *reinterpret_cast<const f32x4 *>(krow + ((half * kQ + i) ^ sw) * 16);
+          const f32x4 x = __builtin_bit_cast(f32x4, q[i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], x[e], s[kb], 0, 0, 0);
+        }
+      }
+    }
+    constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : (uint64_t{1} << (KT % 64)) - 1;
+    const bool masked = k0 + KT - 1 > wmin || (live & kAll) != kAll;
+    // Bit 32 kb + key of the lane's visible keys.
+    uint64_t sees = kAll;
+    if (masked) {
+      const int n = min(limit - k0 + 1, KT);
+      sees = n >= KT ? kAll : n <= 0 ? 0 : (uint64_t{1} << n) - 1;
+      sees &= live;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[kb][i] = sees >> (32 * kb + 8 * (i / 4) + 4 * half + i % 4) & 1 ? s[kb][i] : -FLT_MAX;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb][i]);
+    mx = half_max(mx) * p.scale2;
+    // A maximum that rose by less than 2^8 is left where it is: weights up to 2^8 lose nothing
+    // in float32 sums or in bf16, and the sums need no factor.
+    if (__any(mx > m + 8.f)) {
+      const float mn = fmaxf(m, mx);
+      const float corr = exp2_hw(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= corr;
+      m = mn;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = exp2_hw(fmaf(s[kb][i], p.scale2, -m));
+    if (masked) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[kb][i] = sees >> (32 * kb + 8 * (i / 4) + 4 * half + i % 4) & 1 ? s[kb][i] : 0.f;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) l += s[kb][i];
+
+    // Values.  A key without weight must not reach the sums through a value that is not
+    // finite (zero times it would be NaN): in a tile of which some row does not see
+    // everything such values are taken as zero here, and added to the rows that see them.
+    bool odd = false;
+    if constexpr (kHalf) {
+      // A lane's weights of 16 keys (step c) are keys 16 c + 4 half + 0..3 and 8 further on; the
+      // transposing read gives it feature l32's values of the same ones.
+      u32x4 w[2 * KB];
+#pragma unroll
+      for (int c = 0; c < 2 * KB; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[c][e] = pack_bf16(s[c / 2][8 * (c % 2) + 2 * e], s[c / 2][8 * (c % 2) + 2 * e + 1]);
+      const int vr = 4 * half + lane % 16 / 4;
+      const int vc = lane / 16 % 2 * 2 + lane % 4 / 2;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int c = 0; c < 2 * KB; ++c) {
+          u32x4 v;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int at = 16 * c + 8 * u + vr;
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            const char *from = vt + at * kRowBytes + (((4 * d) ^ Tile::value_swizzle(at)) + vc) * 16 + lane % 2 * 8;
+            const u32x2 x = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
+            v[2 * u] = x[0];
+            v[2 * u + 1] = x[1];
+          }
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool lo = (v[e] & 0x7F80u) == 0x7F80u, hi = (v[e] & 0x7F800000u) == 0x7F800000u;
+              odd |= lo | hi;
+              v[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+            }
+          }
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[c]),
+                                                         o[d], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float *const vrow =
+            reinterpret_cast<const float *>(vt + (8 * (i / 4) + i % 4 + 4 * half) * kRowBytes);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          float v = vrow[32 * d + l32];
+          if (masked) {
+            const bool bad = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
+            odd |= bad;
+            v = bad ? 0.f : v;
+          }
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][i], o[d], 0, 0, 0);
+        }
+      }
+    }
+    if (masked && __any(odd)) {
+      for (int j = 0; j < KT; ++j) {
+        const bool seen = sees >> j & 1;
+        const char *const vrow = vt + j * kRowBytes;
+        const int sw = Tile::value_swizzle(j);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int at = (32 * d + 8 * (i / 4) + 4 * half + i % 4) * static_cast<int>(sizeof(T));   // byte of the row
+            const char *const from = vrow + ((at / 16) ^ sw) * 16 + at % 16;
+            float v;
+            if constexpr (kHalf)
+              v = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(from)) << 16);
+            else
+              v = *reinterpret_cast<const float *>(from);
+            const bool bad = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
+            o[d][i] += seen && bad ? v : 0.f;
+          }
+      }
+    }
+  }
+  if (kPaged && p.err != nullptr && __any(bad_block) && lane == 0) atomicOr(p.err, PRCR_DERR_BLOCK);
+
+  l = half_sum(l);
+  if (!active || wr0 + l32 >= n_rows) return;
+  if (p.n_split > 1) {
+    float *const part = p.part + (row * p.n_split + split) * (D + 2);
+    if (half == 0) {
+      part[D] = m;
+      part[D + 1] = t0 < t1 ? l : 0.f;
+    }
+    if (t0 >= t1) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = 32 * d + 8 * i + 4 * half;
+        *reinterpret_cast<f32x2 *>(part + at) = f32x2{o[d][4 * i], o[d][4 * i + 1]};
+        *reinterpret_cast<f32x2 *>(part + at + 2) = f32x2{o[d][4 * i + 2], o[d][4 * i + 3]};
+      }
+    return;
+  }
+  const float inv = l != 0.f ? 1.f / l : 0.f;   // (a NaN stays one)
+  if (p.lse != nullptr && half == 0)
+    p.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.693147180559945309f : -__builtin_inff();
+  char *const out = static_cast<char *>(p.out) + row * kRowBytes;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = l != 0.f ? o[d][4 * i + e] * inv : 0.f;
+      const int at = 32 * d + 8 * i + 4 * half;
+      if constexpr (kHalf)
+        *reinterpret_cast<u32x2 *>(out + at * 2) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+      else
+        *reinterpret_cast<f32x4 *>(out + at * 4) = x;
+    }
+}
+
+// Merge of a row's partial results: a wave per row, D / 64 features a lane.  Splits without
+// keys have a sum of zero and no features.
+constexpr int kMergeWaves = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(kMergeWaves * kWave) void merge_kernel(const AttendParams p) {
+  constexpr int F = D / kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kMergeWaves + threadIdx.x / kWave;
+  if (row >= static_cast<int64_t>(p.total_q) * p.n_q_heads) return;
+  // Rows of no sequence have no partial results: their token lies behind the sequence's last.
+  const int32_t token = static_cast<int32_t>(row / p.n_q_heads);
+  int lo = 0, n = p.batch;                   // the last sequence that starts at or before the token
+  while (n > 1) {
+    const int step = (n + kWave - 1) / kWave;
+    const int b = lo + lane * step;
+    const bool ok = lane * step < n && p.q_off[b] <= token;
+    const int k = max(__popcll(__ballot(ok)) - 1, 0) * step;
+    lo += k;
+    n = min(step, n - k);
+  }
+  const Rows rows = rows_of(p, lo);
+  if (token < rows.start || token >= rows.start + rows.n) return;
+  const float *const part = p.part + row * p.n_split * (D + 2);
+  float M = -FLT_MAX;
+  for (int s = 0; s < p.n_split; ++s) M = part[s * (D + 2) + D + 1] != 0.f ? fmaxf(M, part[s * (D + 2) + D]) : M;
+  float L = 0.f, O[F] = {};
+  for (int s = 0; s < p.n_split; ++s) {
+    const float ls = part[s * (D + 2) + D + 1];
+    if (ls == 0.f) continue;
+    const float w = exp2_hw(part[s * (D + 2) + D] - M);
+    L += ls * w;
+#pragma unroll
+    for (int f = 0; f < F; ++f) O[f] = fmaf(part[s * (D + 2) + f * kWave + lane], w, O[f]);
+  }
+  if (lane == 0 && p.lse != nullptr)
+    p.lse[row] = L != 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.693147180559945309f : -__builtin_inff();
+#pragma unroll
+  for (int f = 0; f < F; ++f) {
+    const float x = L != 0.f ? O[f] / L : 0.f;
+    if constexpr (sizeof(T) == 2)
+      static_cast<uint16_t *>(p.out)[row * D + f * kWave + lane] = static_cast<uint16_t>(pack_bf16(x, 0.f));
+    else
+      static_cast<float *>(p.out)[row * D + f * kWave + lane] = x;
+  }
+}
+
+template <typename T, int D, bool kPaged>
+hipError_t chunk(const AttendParams &p, const ChunkPlan &plan, hipStream_t stream) {
+  const int64_t blocks = static_cast<int64_t>(p.n_kv_heads) * p.n_slots * p.n_split;
+  const int64_t rows = static_cast<int64_t>(p.total_q) * p.n_q_heads;
+  const int64_t merges = (rows + kMergeWaves - 1) / kMergeWaves;
+  if (blocks > INT32_MAX || !grid_fits(blocks, plan.waves * kWave) || (p.n_split > 1 && !grid_fits(merges, kMergeWaves * kWave)))
+    return hipErrorInvalidConfiguration;
+  if (plan.waves == 1)
+    chunk_kernel<T, D, kPaged, 1><<<static_cast<unsigned>(blocks), kWave, 0, stream>>>(p);
+  else
+    chunk_kernel<T, D, kPaged, 4><<<static_cast<unsigned>(blocks), 4 * kWave, 0, stream>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_split == 1) return e;
+  merge_kernel<T, D><<<static_cast<unsigned>(merges), kMergeWaves * kWave, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+template <typename T, bool kPaged>
+hipError_t chunk_dim(const AttendParams &p, const ChunkPlan &plan, int head_dim, hipStream_t stream) {
+  return head_dim == 64 ? chunk<T, 64, kPaged>(p, plan, stream) : chunk<T, 128, kPaged>(p, plan, stream);
+}
+
+}  // namespace
+
+ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
+                     int32_t head_dim, prcr_dtype dtype) {
+  ChunkPlan plan{};
+  const int64_t group = n_q_heads / n_kv_heads;
+  const int64_t rows = static_cast<int64_t>(total_q) * group;
+  plan.waves = rows <= int64_t{64} * batch ? 1 : 4;
+  plan.n_slots = static_cast<int32_t>(rows / (32 * plan.waves)) + batch;
+  // Enough workgroups for two per compute unit, none of fewer than 256 keys at full capacity.
+  const int64_t have = static_cast<int64_t>(plan.n_slots) * n_kv_heads;
+  const int64_t want = (512 + have - 1) / have, most = (capacity + 255) / 256;
+  plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min(want, most)));
+  const int64_t elem = dtype == PRCR_F32 ? 4 : 2;
+  plan.rotated_bytes = (static_cast<size_t>(total_q) * n_q_heads * head_dim * elem + 255) / 256 * 256;
+  plan.bytes = plan.rotated_bytes;
+  if (plan.n_split > 1) plan.bytes += static_cast<size_t>(total_q) * n_q_heads * plan.n_split * (head_dim + 2) * 4;
+  return plan;
+}
+
+hipError_t launch_chunk(const AttendParams &in, const ChunkPlan &plan, prcr_dtype dtype, int head_dim, bool paged,
+                        hipStream_t stream) {
+  AttendParams p = in;
+  p.n_slots = plan.n_slots;
+  p.n_split = plan.n_split;
+  p.by_split = Divisor::of(plan.n_split);
+  if (dtype == PRCR_F32)
+    return paged ? chunk_dim<float, true>(p, plan, head_dim, stream) : chunk_dim<float, false>(p, plan, head_dim, stream);
+  return paged ? chunk_dim<uint16_t, true>(p, plan, head_dim, stream)
+               : chunk_dim<uint16_t, false>(p, plan, head_dim, stream);
+}
+
+}  // namespace prcr

@@ -553,6 +553,152 @@ PyObject *decode(Args a) {
   return done(st, &failed) ? wrap(out.t) : failed;
 }
 
+// The packed query rows of the operators on several tokens per sequence:
+// (q, q_off, q_pos, cache_len, q_len)
+struct QueryRows {
+  QueryRows(const Store &cache, PyObject *q_, PyObject *off_, PyObject *pos_, PyObject *len_, PyObject *rows_)
+      : q(tensor(q_)), off(tensor(off_)), pos(tensor(pos_)), cache_len(tensor(len_)), len(tensor_or_none(rows_)) {
+    if (q.dim() != 3) throw Skip();
+    need(q, cache.k.scalar_type(), cache.device, {q.size(0), q.size(1), cache.k.size(4)});
+    need(off, at::kInt, cache.device, {cache.rows() + 1});
+    need(pos, at::kInt, cache.device, {q.size(0), 3});
+    need(cache_len, at::kInt, cache.device, {cache.rows()});
+    if (len.defined()) need(len, at::kInt, cache.device, {cache.rows()});
+    total = to_int32(q.size(0));
+    heads = to_int32(q.size(1));
+  }
+  at::Tensor q, off, pos, cache_len, len;
+  int32_t total, heads;
+};
+
+int64_t capacity_of(const Store &c) {
+  return c.paged ? static_cast<int64_t>(c.c.max_blocks) * c.c.block_size : int64_t{c.c.s_max};
+}
+
+// A call's workspace: the caller's, checked, or one made here (inside Unlocked).
+struct Workspace {
+  Workspace(PyObject *o, at::Device device, size_t bytes_) : t(tensor_or_none(o)), bytes(bytes_) {
+    if (!t.defined()) return;
+    need(t, device);
+    if (t.nbytes() < bytes) throw Skip();
+  }
+  void make(const Launch &on) {
+    if (!t.defined())
+      t = on.fresh({static_cast<int64_t>((std::max(bytes, size_t{4}) + 3) / 4)}, at::kFloat, false);
+  }
+  at::Tensor t;
+  size_t bytes;
+};
+
+// (rope, cache, layer, q, q_off, q_pos, cache_len, q_len, scale, out, lse, workspace, err, stream)
+PyObject *chunk_attention(Args a) {
+  const prcr_rope rope = rope_of(a[0]);
+  const Store cache(a[1]);
+  const int32_t layer = int32_of(a[2]);
+  const QueryRows rows(cache, a[3], a[4], a[5], a[6], a[7]);
+  const int64_t T = rows.total, Hq = rows.heads, D = cache.k.size(4);
+  const double scale = a[8] == Py_None ? std::pow(static_cast<double>(D), -0.5) : double_of(a[8]);
+  Out out(a[9], cache.k.scalar_type(), cache.device, {T, Hq, D}), lse(a[10], at::kFloat, cache.device, {T, Hq});
+  const prcr_dtype dtype = dtype_of(cache.k);
+  const int32_t b = to_int32(cache.rows()), nl = to_int32(cache.n_layers()), h = to_int32(cache.n_kv_heads());
+  size_t bytes = 0;
+  if (prcr_chunk_workspace_size(&cache.c, dtype, b, rows.total, rows.heads, h, to_int32(D), &bytes) != PRCR_OK)
+    throw Skip();
+  Workspace ws(a[11], cache.device, bytes);
+  const at::Tensor err = err_of(a[12], cache.device);
+  const Launch on(a[13], cache.device);
+  prcr_status st;
+  {
+    Unlocked u;
+    out.make(on);
+    lse.make(on);
+    ws.make(on);
+    st = prcr_chunk_attention(&rope, &cache.c, dtype, b, nl, h, layer, ptr<void>(rows.q), rows.heads,
+                              ptr<int32_t>(rows.off), ptr<int32_t>(rows.len), rows.total, ptr<int32_t>(rows.pos),
+                              ptr<int32_t>(rows.cache_len), static_cast<float>(scale), ptr<void>(out.t),
+                              ptr<float>(lse.t), ptr<void>(ws.t), ws.t.nbytes(), ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? tuple_of(out.t, lse.t) : failed;
+}
+
+// (rope, cache, layer, q, q_off, q_pos, cache_len, lse, q_len, window, scale, weights, accumulate,
+//  workspace, err, stream)
+PyObject *key_weights(Args a) {
+  const prcr_rope rope = rope_of(a[0]);
+  const Store cache(a[1]);
+  const int32_t layer = int32_of(a[2]);
+  const QueryRows rows(cache, a[3], a[4], a[5], a[6], a[8]);
+  const at::Tensor lse = tensor(a[7]);
+  const int64_t T = rows.total, Hq = rows.heads, D = cache.k.size(4);
+  need(lse, at::kFloat, cache.device, {T, Hq});
+  const int32_t window = a[9] == Py_None ? 0 : int32_of(a[9]);
+  if (a[9] != Py_None && window < 1) throw Skip();
+  const double scale = a[10] == Py_None ? std::pow(static_cast<double>(D), -0.5) : double_of(a[10]);
+  Out weights(a[11], at::kFloat, cache.device, {cache.rows(), cache.n_kv_heads(), capacity_of(cache)});
+  const bool accumulate = bool_of(a[12]);
+  if (accumulate && !weights.t.defined()) throw Skip();
+  const prcr_dtype dtype = dtype_of(cache.k);
+  const int32_t b = to_int32(cache.rows()), nl = to_int32(cache.n_layers()), h = to_int32(cache.n_kv_heads());
+  size_t bytes = 0;
+  if (prcr_key_weights_workspace_size(dtype, rows.total, rows.heads, to_int32(D), &bytes) != PRCR_OK) throw Skip();
+  Workspace ws(a[13], cache.device, bytes);
+  const at::Tensor err = err_of(a[14], cache.device);
+  const Launch on(a[15], cache.device);
+  prcr_status st;
+  {
+    Unlocked u;
+    weights.make(on);
+    ws.make(on);
+    st = prcr_key_weights(&rope, &cache.c, dtype, b, nl, h, layer, ptr<void>(rows.q), rows.heads,
+                          ptr<int32_t>(rows.off), ptr<int32_t>(rows.len), rows.total, ptr<int32_t>(rows.pos),
+                          ptr<int32_t>(rows.cache_len), ptr<float>(lse), window, static_cast<float>(scale),
+                          accumulate ? 1 : 0, ptr<float>(weights.t), ptr<void>(ws.t), ws.t.nbytes(),
+                          ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? wrap(weights.t) : failed;
+}
+
+// (cache, cache_len, weights, budget, keep_first, keep_last, mem, new_cache_len, kept, new_weights,
+//  workspace, err, stream)
+PyObject *evict(Args a) {
+  const Store cache(a[0]);
+  const at::Tensor cache_len = tensor(a[1]), weights = tensor(a[2]);
+  const int64_t B = cache.rows(), H = cache.n_kv_heads(), cap = capacity_of(cache);
+  need(cache_len, at::kInt, cache.device, {B});
+  need(weights, at::kFloat, cache.device, {B, H, cap});
+  const int32_t budget = int32_of(a[3]), first = int32_of(a[4]), last = int32_of(a[5]);
+  std::optional<Mem> mem;
+  if (a[6] != Py_None) {
+    mem.emplace(a[6]);
+    if (mem->device != cache.device) throw Skip();
+  }
+  Out new_len(a[7], at::kInt, cache.device, {B}), kept(a[8], at::kInt, cache.device, {B, budget}),
+      new_weights(a[9], at::kFloat, cache.device, {B, H, cap});
+  const prcr_dtype dtype = dtype_of(cache.k);
+  const int32_t b = to_int32(B), nl = to_int32(cache.n_layers()), h = to_int32(H);
+  size_t bytes = 0;
+  if (budget < 1 || prcr_evict_workspace_size(&cache.c, b, &bytes) != PRCR_OK) throw Skip();
+  Workspace ws(a[10], cache.device, bytes);
+  const at::Tensor err = err_of(a[11], cache.device);
+  const Launch on(a[12], cache.device);
+  prcr_status st;
+  {
+    Unlocked u;
+    new_len.make(on);
+    kept.make(on);
+    new_weights.make(on);
+    ws.make(on);
+    st = prcr_evict(&cache.c, dtype, b, nl, h, to_int32(cache.k.size(4)), ptr<int32_t>(cache_len),
+                    ptr<float>(weights), budget, first, last, ptr<int32_t>(new_len.t), ptr<int32_t>(kept.t),
+                    ptr<float>(new_weights.t), mem ? &mem->c : nullptr, ptr<void>(ws.t), ws.t.nbytes(),
+                    ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? tuple_of(new_len.t, kept.t, new_weights.t) : failed;
+}
+
 // (Rope, Memory, Cache, MODES), once.
 PyObject *setup(PyObject *, Args a, Py_ssize_t n) {
   if (n != 4 || !PyDict_CheckExact(a[3])) {
@@ -575,6 +721,9 @@ PyMethodDef methods[] = {
     PRCR_ENTRY(prefill_capture, 13, prefill_capture),
     PRCR_ENTRY(decode_attention, 11, decode<false>),
     PRCR_ENTRY(decode_attention_static, 10, decode<true>),
+    PRCR_ENTRY(chunk_attention, 14, chunk_attention),
+    PRCR_ENTRY(key_weights, 16, key_weights),
+    PRCR_ENTRY(evict, 13, evict),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_prcr_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
