@@ -69,12 +69,13 @@ struct TileOf {
 };
 
 template <typename T, int D, bool kPaged, int kWaves>
-__global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendParams p) {
+__global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_kernel(const AttendParams p) {
   using Tile = TileOf<T, D>;
   constexpr bool kHalf = sizeof(T) == 2;     // bf16
   constexpr int M = 32 * kWaves;
   constexpr int KT = Tile::kKeys, kRowBytes = Tile::kRowBytes;
   constexpr int KB = KT / 32;                // key blocks of a tile
+  constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : (uint64_t{1} << (KT % 64)) - 1;
   constexpr int DT = D / 32;                 // feature blocks
   constexpr int kMine = Tile::kLoads / kWaves;   // loads of each operand per wave and tile
   __shared__ __align__(1024) char s_kv[2][2][Tile::kBytes];
@@ -103,14 +104,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
   const int per = (n_tiles + p.n_split - 1) / p.n_split;
   const int t0 = min(split * per, n_tiles), t1 = min(t0 + per, n_tiles);
 
-  // The lane's row, and the last slots that it, the wave's first row and its last one see.
+  // The lane's row, and the last slots that it and the wave's last row see.
   const int wr0 = r0 + wave * 32;
   const bool active = wr0 < n_rows;
   const int r = min(wr0 + l32, n_rows - 1);
   const int token = token_of(r);
   const int64_t row = (static_cast<int64_t>(rows.start) + token) * p.n_q_heads + kvh * G + (r - token * G);
   const int limit = first + token;
-  const int wmin = __builtin_amdgcn_readfirstlane(limit);
   const int wmax = __builtin_amdgcn_readlane(limit, 31);
 
   // Query operand.  bf16: of product kk, elements 16 kk + 8 half + 0..7.  float32: the
@@ -184,7 +184,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
     live_next = load_tile(t0, s_kv[t0 & 1]);
     if constexpr (kPaged) entry = entry_of(min(t0 + 1, t1 - 1), &entry_off);
   }
-  for (int t = t0; t < t1; ++t) {
+  // One tile.  The first tiles, which every row sees whole, have neither the mask nor, between
+  // their reads and products, what is done for it: kMasked is right for every tile.
+  auto step = [&](int t, auto is_masked) {
+    constexpr bool kMasked = decltype(is_masked)::value;
     // The tile's loads have arrived, in every wave, and every wave is done with the other buffer.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -194,7 +197,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
       if constexpr (kPaged) entry = entry_of(min(t + 2, t1 - 1), &entry_off);
     }
     const int k0 = t * KT;
-    if (!active || k0 > wmax) continue;
+    if (!active || (kMasked && k0 > wmax)) return;
     const char *const kt = s_kv[t & 1][0];
     const char *const vt = s_kv[t & 1][1];
 
@@ -220,19 +223,19 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
         }
       }
     }
-    constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : (uint64_t{1} << (KT % 64)) - 1;
-    const bool masked = k0 + KT - 1 > wmin || (live & kAll) != kAll;
-    // Bit 32 kb + key of the lane's visible keys.
-    uint64_t sees = kAll;
-    if (masked) {
+    uint64_t sees = kAll;                  // bit: key of the tile that the lane's row sees
+    uint32_t mine[2] = {~0u, ~0u};         // from the lane's first key on
+    auto seen = [&](int kb, int i) -> bool { return mine[kb] >> (8 * (i / 4) + i % 4) & 1; };
+    if constexpr (kMasked) {
       const int n = min(limit - k0 + 1, KT);
       sees = n >= KT ? kAll : n <= 0 ? 0 : (uint64_t{1} << n) - 1;
       sees &= live;
+      mine[0] = static_cast<uint32_t>(sees) >> (4 * half);
+      mine[1] = static_cast<uint32_t>(sees >> 32) >> (4 * half);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          s[kb][i] = sees >> (32 * kb + 8 * (i / 4) + 4 * half + i % 4) & 1 ? s[kb][i] : -FLT_MAX;
+        for (int i = 0; i < 16; ++i) s[kb][i] = seen(kb, i) ? s[kb][i] : -FLT_MAX;
     }
     float mx = s[0][0];
 #pragma unroll
@@ -255,18 +258,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = exp2_hw(fmaf(s[kb][i], p.scale2, -m));
-    if (masked) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          s[kb][i] = sees >> (32 * kb + 8 * (i / 4) + 4 * half + i % 4) & 1 ? s[kb][i] : 0.f;
-    }
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) l += s[kb][i];
+      for (int i = 0; i < 16; ++i) {
+        s[kb][i] = exp2_hw(fmaf(s[kb][i], p.scale2, -m));
+        if constexpr (kMasked) s[kb][i] = seen(kb, i) ? s[kb][i] : 0.f;
+        l += s[kb][i];
+      }
 
     // Values.  A key without weight must not reach the sums through a value that is not
     // finite (zero times it would be NaN): in a tile of which some row does not see
@@ -279,35 +275,48 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
 #pragma unroll
       for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[c][e] = pack_bf16(s[c / 2][8 * (c % 2) + 2 * e], s[c / 2][8 * (c % 2) + 2 * e + 1]);
-      const int vr = 4 * half + lane % 16 / 4;
-      const int vc = lane / 16 % 2 * 2 + lane % 4 / 2;
+        for (int e = 0; e < 4; ++e)
+          w[c][e] = pack_bf16(s[c / 2][8 * (c % 2) + 2 * e], s[c / 2][8 * (c % 2) + 2 * e + 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      const int x = lane % 16 / 4;
+      const char *const vrow = vt + (4 * half + x) * kRowBytes + (lane / 16 % 2 * 2 + lane % 4 / 2) * 16 + lane % 2 * 8;
+      // Feature block d's operands: one block's reads are in flight while the last one's
+      // products run (the compiler left to itself reads all of them first, and spills).
+      auto read = [&](int d, u32x4 (&v)[2 * KB]) {
+        const char *const at = vrow + ((4 * d) ^ Tile::value_swizzle(x)) * 16;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int c = 0; c < 2 * KB; ++c) {
-          u32x4 v;
+        for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const int at = 16 * c + 8 * u + vr;
             typedef short s16x4 __attribute__((ext_vector_type(4)));
-            const char *from = vt + at * kRowBytes + (((4 * d) ^ Tile::value_swizzle(at)) + vc) * 16 + lane % 2 * 8;
-            const u32x2 x = __builtin_bit_cast(
-                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from));
-            v[2 * u] = x[0];
-            v[2 * u + 1] = x[1];
+            const u32x2 two = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4 *)(at + (16 * c + 8 * u) * kRowBytes)));
+            v[c][2 * u] = two[0];
+            v[c][2 * u + 1] = two[1];
           }
-          if (masked) {
+      };
+      u32x4 v[2][2 * KB];
+      read(0, v[0]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        if (d + 1 < DT) read(d + 1, v[(d + 1) % 2]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < 2 * KB; ++c) {
+          u32x4 &a = v[d % 2][c];
+          if constexpr (kMasked) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const bool lo = (v[e] & 0x7F80u) == 0x7F80u, hi = (v[e] & 0x7F800000u) == 0x7F800000u;
+              const bool lo = (a[e] & 0x7F80u) == 0x7F80u, hi = (a[e] & 0x7F800000u) == 0x7F800000u;
               odd |= lo | hi;
-              v[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+              a[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
             }
           }
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[c]),
-                                                         o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                         __builtin_bit_cast(bf16x8, w[c]), o[d], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -316,7 +325,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           float v = vrow[32 * d + l32];
-          if (masked) {
+          if constexpr (kMasked) {
             const bool bad = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
             odd |= bad;
             v = bad ? 0.f : v;
@@ -325,9 +334,9 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
         }
       }
     }
-    if (masked && __any(odd)) {
+    if (kMasked && __any(odd)) {
       for (int j = 0; j < KT; ++j) {
-        const bool seen = sees >> j & 1;
+        const bool in = sees >> j & 1;
         const char *const vrow = vt + j * kRowBytes;
         const int sw = Tile::value_swizzle(j);
 #pragma unroll
@@ -342,11 +351,19 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void chunk_kernel(const AttendPa
             else
               v = *reinterpret_cast<const float *>(from);
             const bool bad = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
-            o[d][i] += seen && bad ? v : 0.f;
+            o[d][i] += in && bad ? v : 0.f;
           }
       }
     }
+  };
+  // Tiles that the workgroup's first row sees whole.
+  const int t_whole = min(t1, max(t0, (first + token_of(r0) + 1) / KT));
+  int t = t0;
+  for (; t < t_whole; ++t) {
+    if (kPaged && (live_next & kAll) != kAll) break;                                // (a block outside the pool; the same in every wave)
+    step(t, std::false_type{});
   }
+  for (; t < t1; ++t) step(t, std::true_type{});
   if (kPaged && p.err != nullptr && __any(bad_block) && lane == 0) atomicOr(p.err, PRCR_DERR_BLOCK);
 
   l = half_sum(l);
