@@ -442,9 +442,11 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache,
                              void *workspace, size_t workspace_bytes, int32_t *err_flag,
                              hipStream_t stream);
 
-/* Workspace bytes prcr_key_weights needs (host). */
-prcr_status prcr_key_weights_workspace_size(prcr_dtype dtype, int32_t total_q,
-                                            int32_t n_q_heads, int32_t head_dim,
+/* Workspace bytes prcr_key_weights needs for this cache, shape and window (host). */
+prcr_status prcr_key_weights_workspace_size(const prcr_cache *cache, prcr_dtype dtype,
+                                            int32_t batch, int32_t total_q,
+                                            int32_t n_q_heads, int32_t n_kv_heads,
+                                            int32_t head_dim, int32_t window,
                                             size_t *bytes);
 
 /*

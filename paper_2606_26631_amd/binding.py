@@ -118,7 +118,8 @@ def lib() -> ctypes.CDLL:
                                        c_int32, c_void_p, c_void_p, ctypes.c_float, c_void_p,
                                        c_void_p, c_void_p, ctypes.c_size_t, c_void_p, c_void_p]
     L.prcr_key_weights_workspace_size.restype = c_int
-    L.prcr_key_weights_workspace_size.argtypes = [c_int, c_int32, c_int32, c_int32,
+    L.prcr_key_weights_workspace_size.argtypes = [POINTER(CCache), c_int, c_int32, c_int32, c_int32,
+                                                  c_int32, c_int32, c_int32,
                                                   POINTER(ctypes.c_size_t)]
     L.prcr_key_weights.restype = c_int
     L.prcr_key_weights.argtypes = [POINTER(CRope), POINTER(CCache), c_int, c_int32, c_int32, c_int32,
@@ -740,10 +741,12 @@ def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache
     return out, lse
 
 
-def key_weights_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int) -> int:
+def key_weights_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int, window=None) -> int:
     """Bytes of workspace prcr_key_weights needs (prcr_key_weights_workspace_size)."""
-    return _size_t("prcr_key_weights_workspace_size", _dtype_code(cache.k), int(total_q), int(n_q_heads),
-                   int(_cache_dims(cache)[2]))
+    NL, H, D = _cache_dims(cache)
+    return _size_t("prcr_key_weights_workspace_size", ctypes.byref(cache.to_c()), _dtype_code(cache.k),
+                   _batch(cache), int(total_q), int(n_q_heads), int(H), int(D),
+                   0 if window is None else int(window))
 
 
 def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len, lse, q_len=None,
@@ -769,7 +772,7 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
         weights = _new((B, H, _capacity(cache)), torch.float32, cache.device, stream)
     _need(weights, "weights", torch.float32, 3, cache.device)
     _shape(weights, "weights", (B, H, _capacity(cache)))
-    workspace = _workspace(workspace, key_weights_workspace_bytes(cache, T, Hq), cache.device, stream)
+    workspace = _workspace(workspace, key_weights_workspace_bytes(cache, T, Hq, window), cache.device, stream)
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
     st = lib().prcr_key_weights(

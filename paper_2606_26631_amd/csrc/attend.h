@@ -26,20 +26,22 @@ struct AttendParams {
   const int32_t *block_table;
   void *out;                      // chunk attention: [total_q][n_q_heads][head_dim]
   float *lse;                     // [total_q][n_q_heads]: out (or null), or the weights' input
-  float *part;                    // chunk attention: [total_q][n_q_heads][n_split][head_dim + 2]
+  float *part;                    // chunk attention: [total_q][n_q_heads][n_split][head_dim + 2];
+                                  // weights: [n_split][batch][n_kv_heads][capacity]
   float *weights;                 // weights: [batch][n_kv_heads][capacity]
   int32_t *err;
   int32_t total_q, batch, n_layers, n_kv_heads, n_q_heads, group, layer;
   int32_t s_max, block_size, max_blocks, n_blocks;
   int32_t block_shift;            // log2(block_size) if a power of two, else -1
   int32_t capacity;               // slots per sequence: s_max, or max_blocks * block_size
-  int32_t n_slots, n_split;       // chunk attention: row tiles there is room for, key splits (launcher)
+  int32_t n_slots, n_split;       // chunk attention: row tiles there is room for, key splits;
+                                  // weights: key stretches of a sequence, row splits (launcher)
   int32_t window;                 // weights: the last rows of each sequence that count (0: all)
   int32_t accumulate;
   float scale;                    // |scale|; a negative one turns the rotated queries' sign
   float scale2;                   // |scale| log2(e)
   int32_t negate;
-  Divisor by_group, by_heads, by_split;
+  Divisor by_group, by_heads, by_split, by_slot;
   int8_t axis[kMaxPairs];
   double inv_freq[kMaxPairs];
 };
@@ -71,10 +73,20 @@ struct ChunkPlan {
 ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
                      int32_t head_dim, prcr_dtype dtype);
 
+// The same of the keys' weights: 32-key blocks a wave holds, key stretches of a sequence, and
+// the workgroups that share a stretch's rows.
+struct WeightsPlan {
+  int32_t blocks, n_stretches, n_split;
+  size_t rotated_bytes, bytes;
+};
+WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
+                             int32_t head_dim, int32_t window, prcr_dtype dtype);
+
 hipError_t launch_rotate(const AttendParams &p, prcr_dtype dtype, int head_dim, hipStream_t stream);
 hipError_t launch_chunk(const AttendParams &p, const ChunkPlan &plan, prcr_dtype dtype, int head_dim, bool paged,
                         hipStream_t stream);
-hipError_t launch_key_weights(const AttendParams &p, prcr_dtype dtype, int head_dim, bool paged, hipStream_t stream);
+hipError_t launch_key_weights(const AttendParams &p, const WeightsPlan &plan, prcr_dtype dtype, int head_dim, bool paged,
+                              hipStream_t stream);
 hipError_t launch_evict(const EvictParams &p, bool paged, hipStream_t stream);
 
 #ifdef __HIPCC__

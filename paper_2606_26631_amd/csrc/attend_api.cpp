@@ -197,14 +197,18 @@ prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,
   return launch_status(launch_chunk(p, plan, dtype, rope->head_dim, cache->paged != 0, stream));
 }
 
-prcr_status prcr_key_weights_workspace_size(prcr_dtype dtype, int32_t total_q, int32_t n_q_heads, int32_t head_dim,
+prcr_status prcr_key_weights_workspace_size(const prcr_cache *cache, prcr_dtype dtype, int32_t batch, int32_t total_q,
+                                            int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t window,
                                             size_t *bytes) {
   if (bytes == nullptr) return PRCR_ERR_NULL;
   if (dtype != PRCR_F32 && dtype != PRCR_BF16) return PRCR_ERR_DTYPE;
-  prcr_status st = check_heads(1, 1, head_dim);
-  if (st == PRCR_OK) st = check_rows(total_q, n_q_heads, 1);
+  int64_t capacity = 0;
+  prcr_status st = check_heads(batch, n_kv_heads, head_dim);
+  if (st == PRCR_OK) st = check_rows(total_q, n_q_heads, n_kv_heads);
+  if (st == PRCR_OK) st = cache_shape(cache, &capacity);
+  if (st == PRCR_OK && window < 0) st = PRCR_ERR_SHAPE;
   if (st != PRCR_OK) return st;
-  *bytes = static_cast<size_t>(total_q) * n_q_heads * head_dim * elem_bytes(dtype);
+  *bytes = plan_key_weights(capacity, batch, total_q, n_q_heads, n_kv_heads, head_dim, window, dtype).bytes;
   return PRCR_OK;
 }
 
@@ -221,16 +225,18 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache, prc
   if (weights == nullptr || (total_q > 0 && lse == nullptr)) return PRCR_ERR_NULL;
   if (window < 0) return PRCR_ERR_SHAPE;
   const double row_bytes = static_cast<double>(rope->head_dim) * elem_bytes(dtype), rows = static_cast<double>(total_q) * n_q_heads;
-  if (static_cast<double>(workspace_bytes) < rows * row_bytes) return PRCR_ERR_SHAPE;
+  const WeightsPlan plan = plan_key_weights(p.capacity, batch, total_q, n_q_heads, n_kv_heads, rope->head_dim, window, dtype);
+  if (workspace_bytes < plan.bytes) return PRCR_ERR_SHAPE;
   if (!aligned(weights, 4) || !aligned(lse, 4)) return PRCR_ERR_ALIGN;
   const double all = cache_bytes(*cache, batch, n_layers, n_kv_heads, row_bytes);
-  const Range written[] = {{weights, 4.0 * batch * n_kv_heads * p.capacity}, {workspace, rows * row_bytes}};
+  const Range written[] = {{weights, 4.0 * batch * n_kv_heads * p.capacity}, {workspace, static_cast<double>(plan.bytes)}};
   const Range read[] = {{q, rows * row_bytes}, {lse, rows * 4}, {q_off, (batch + 1) * 4.0}, {q_len, batch * 4.0},
                         {q_pos, total_q * 12.0}, {cache_len, batch * 4.0}, {cache->k, all}, {cache->v, all},
                         {cache->paged ? cache->block_table : nullptr, 4.0 * batch * cache->max_blocks}};
   if (aliases(written, read)) return PRCR_ERR_ALIAS;
   p.lse = const_cast<float *>(lse);
   p.weights = weights;
+  p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.rotated_bytes);
   p.window = window;
   p.accumulate = accumulate != 0;
   if (total_q > 0) {
@@ -239,7 +245,7 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache, prc
   } else if (p.accumulate) {
     return PRCR_OK;                          // no row gives any weight
   }
-  return launch_status(launch_key_weights(p, dtype, rope->head_dim, cache->paged != 0, stream));
+  return launch_status(launch_key_weights(p, plan, dtype, rope->head_dim, cache->paged != 0, stream));
 }
 
 prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch, size_t *bytes) {

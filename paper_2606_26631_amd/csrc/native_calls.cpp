@@ -641,7 +641,9 @@ PyObject *key_weights(Args a) {
   const prcr_dtype dtype = dtype_of(cache.k);
   const int32_t b = to_int32(cache.rows()), nl = to_int32(cache.n_layers()), h = to_int32(cache.n_kv_heads());
   size_t bytes = 0;
-  if (prcr_key_weights_workspace_size(dtype, rows.total, rows.heads, to_int32(D), &bytes) != PRCR_OK) throw Skip();
+  if (prcr_key_weights_workspace_size(&cache.c, dtype, b, rows.total, rows.heads, h, to_int32(D), window, &bytes) !=
+      PRCR_OK)
+    throw Skip();
   Workspace ws(a[13], cache.device, bytes);
   const at::Tensor err = err_of(a[14], cache.device);
   const Launch on(a[15], cache.device);
