@@ -394,7 +394,7 @@ prcr_status prcr_decode_attention_static(const prcr_rope *rope, const prcr_cache
  *
  *   out           [total_q][n_q_heads][head_dim], dtype, 16-byte aligned
  *   lse           float32 [total_q][n_q_heads], or NULL
- *   workspace     prcr_chunk_workspace_size() bytes, 16-byte aligned
+ *   workspace     prcr_chunk_workspace_size() bytes, 16-byte aligned (NULL where that is 0)
  * Scores, the softmax and the sums are float32; bfloat16 weights are rounded to
  * bfloat16 for the product with the values (their sum is taken before that), and out is rounded once.  A row
  * that sees no slot gets out = 0 and lse = -infinity.  Values and keys at slots that a row
@@ -412,8 +412,8 @@ prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,
                                  hipStream_t stream);
 
 /* Workspace bytes prcr_chunk_attention needs for this cache and shape (host). */
-prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, prcr_dtype dtype,
-                                      int32_t batch, int32_t total_q, int32_t n_q_heads,
+prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, int32_t batch,
+                                      int32_t total_q, int32_t n_q_heads,
                                       int32_t n_kv_heads, int32_t head_dim, size_t *bytes);
 
 /*

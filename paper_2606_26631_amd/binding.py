@@ -110,7 +110,7 @@ def lib() -> ctypes.CDLL:
                                c_int, c_int32, POINTER(CCache), c_void_p, c_void_p, c_void_p,
                                c_void_p, c_void_p, c_void_p, c_void_p]
     L.prcr_chunk_workspace_size.restype = c_int
-    L.prcr_chunk_workspace_size.argtypes = [POINTER(CCache), c_int, c_int32, c_int32, c_int32, c_int32,
+    L.prcr_chunk_workspace_size.argtypes = [POINTER(CCache), c_int32, c_int32, c_int32, c_int32,
                                             c_int32, POINTER(ctypes.c_size_t)]
     L.prcr_chunk_attention.restype = c_int
     L.prcr_chunk_attention.argtypes = [POINTER(CRope), POINTER(CCache), c_int, c_int32, c_int32,
@@ -703,8 +703,8 @@ def _query_rows(cache: Cache, q, q_off, q_pos, cache_len, q_len):
 def chunk_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int) -> int:
     """Bytes of workspace prcr_chunk_attention needs (prcr_chunk_workspace_size)."""
     NL, H, D = _cache_dims(cache)
-    return _size_t("prcr_chunk_workspace_size", ctypes.byref(cache.to_c()), _dtype_code(cache.k),
-                   _batch(cache), int(total_q), int(n_q_heads), int(H), int(D))
+    return _size_t("prcr_chunk_workspace_size", ctypes.byref(cache.to_c()), _batch(cache), int(total_q),
+                   int(n_q_heads), int(H), int(D))
 
 
 def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len, q_len=None,

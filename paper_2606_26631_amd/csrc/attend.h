@@ -16,7 +16,7 @@ namespace prcr {
 // sequence's rows are q_off[b] .. q_off[b + 1] - 1, or the first q_len[b] of them.
 struct AttendParams {
   const void *q;                  // [total_q][n_q_heads][head_dim], as given
-  void *rotated;                  // the same, rotated (workspace)
+  void *rotated;                  // weights: the same, rotated (workspace)
   const int32_t *q_off;           // [batch + 1]
   const int32_t *q_len;           // [batch] or null
   const int32_t *q_pos;           // [total_q][3]
@@ -41,7 +41,7 @@ struct AttendParams {
   float scale;                    // |scale|; a negative one turns the rotated queries' sign
   float scale2;                   // |scale| log2(e)
   int32_t negate;
-  Divisor by_group, by_heads, by_split, by_slot;
+  Divisor by_group, by_heads, by_split, by_slot, by_row;
   int8_t axis[kMaxPairs];
   double inv_freq[kMaxPairs];
 };
@@ -64,16 +64,16 @@ struct EvictParams {
 };
 
 // What a call of chunk attention needs besides its arguments: how its rows and keys are
-// divided, and the bytes of its workspace (rotated queries, then partial results).
+// divided, and the bytes of its workspace (partial results of several splits).
 struct ChunkPlan {
   int32_t waves;                  // per workgroup: a tile is 32 rows a wave
   int32_t n_slots, n_split;
-  size_t rotated_bytes, bytes;
+  size_t bytes;
 };
 ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
-                     int32_t head_dim, prcr_dtype dtype);
+                     int32_t head_dim);
 
-// The same of the keys' weights: 32-key blocks a wave holds, key stretches of a sequence, and
+// The same of the keys' weights (rotated queries, then partial sums): 32-key blocks a wave holds, key stretches of a sequence, and
 // the workgroups that share a stretch's rows.
 struct WeightsPlan {
   int32_t blocks, n_stretches, n_split;
@@ -131,9 +131,61 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return half_max(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) x += __shfl_xor(x, d);
+  return half_sum(x);
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {   // to nearest, ties to even
   const f32x2 x = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
+// sin and cos of an angle, to about 2^-52.  The angle less the
+// nearest multiple of pi/2 (kept as two doubles, one fused multiply-add each: Cody and Waite's
+// reduction), then the Taylor series on [-pi/4, pi/4]; its terms of degree 17 and 18 are below
+// 2^-54.  The math library's sincos, made for any double, took 10 us in a launch of a few waves.
+__device__ __forceinline__ void turn(double x, double *sn, double *cs) {
+  const double n = rint(x * 0.63661977236758134308);
+  const double r = fma(-n, 6.12323399573676603587e-17, fma(-n, 1.57079632679489655800, x));
+  const double z = r * r;
+  double s = -1. / 1307674368000., c = 1. / 20922789888000.;
+  s = fma(s, z, 1. / 6227020800.);
+  c = fma(c, z, -1. / 87178291200.);
+  s = fma(s, z, -1. / 39916800.);
+  c = fma(c, z, 1. / 479001600.);
+  s = fma(s, z, 1. / 362880.);
+  c = fma(c, z, -1. / 3628800.);
+  s = fma(s, z, -1. / 5040.);
+  c = fma(c, z, 1. / 40320.);
+  s = fma(s, z, 1. / 120.);
+  c = fma(c, z, -1. / 720.);
+  s = fma(s, z, -1. / 6.);
+  c = fma(c, z, 1. / 24.);
+  s = fma(s * z, r, r);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.);
+  const int q = static_cast<int>(fma(-4., floor(n * 0.25), n));   // n modulo 4
+  const double a = q & 1 ? c : s, b = q & 1 ? s : c;
+  *sn = q & 2 ? -a : a;
+  *cs = (q + 1) & 2 ? -b : b;
+}
+
+// Reports what is wrong with the offsets and lengths, which the kernels only skip.
+__device__ __forceinline__ void report(const AttendParams &p, int thread, int threads) {
+  int bits = 0;
+  for (int b = thread; b < p.batch; b += threads) {
+    if (rows_of(p, b).bad) bits |= PRCR_DERR_OFFSETS;
+    const int32_t len = p.cache_len[b];
+    if (len != clamp_length(len, p.capacity)) bits |= PRCR_DERR_CAPACITY;
+  }
+  if (bits != 0) atomicOr(p.err, bits);
 }
 
 }  // namespace

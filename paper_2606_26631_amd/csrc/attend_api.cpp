@@ -92,7 +92,7 @@ prcr_status prepare(const prcr_rope *rope, const prcr_cache *cache, prcr_dtype d
   int64_t capacity = 0;
   if ((st = check_cache(cache, &capacity)) != PRCR_OK) return st;
   if (q_off == nullptr || cache_len == nullptr) return PRCR_ERR_NULL;
-  if (total_q > 0 && (q == nullptr || q_pos == nullptr || workspace == nullptr)) return PRCR_ERR_NULL;
+  if (total_q > 0 && (q == nullptr || q_pos == nullptr)) return PRCR_ERR_NULL;
   if (n_layers < 1 || layer < 0 || layer >= n_layers || !std::isfinite(scale)) return PRCR_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(q_off, 4) || !aligned(q_len, 4) || !aligned(q_pos, 4) || !aligned(cache_len, 4) ||
       !aligned(workspace, 16) || !aligned(err_flag, 4))
@@ -155,16 +155,15 @@ bool aliases(const Range (&written)[kWritten], const Range (&read)[kRead]) {
 
 extern "C" {
 
-prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, prcr_dtype dtype, int32_t batch, int32_t total_q,
-                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, size_t *bytes) {
+prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, int32_t batch, int32_t total_q, int32_t n_q_heads,
+                                      int32_t n_kv_heads, int32_t head_dim, size_t *bytes) {
   if (bytes == nullptr) return PRCR_ERR_NULL;
-  if (dtype != PRCR_F32 && dtype != PRCR_BF16) return PRCR_ERR_DTYPE;
   int64_t capacity = 0;
   prcr_status st = check_heads(batch, n_kv_heads, head_dim);
   if (st == PRCR_OK) st = check_rows(total_q, n_q_heads, n_kv_heads);
   if (st == PRCR_OK) st = cache_shape(cache, &capacity);
   if (st != PRCR_OK) return st;
-  *bytes = plan_chunk(capacity, batch, total_q, n_q_heads, n_kv_heads, head_dim, dtype).bytes;
+  *bytes = plan_chunk(capacity, batch, total_q, n_q_heads, n_kv_heads, head_dim).bytes;
   return PRCR_OK;
 }
 
@@ -179,7 +178,8 @@ prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,
   if (st != PRCR_OK) return st;
   if (total_q == 0) return PRCR_OK;
   if (out == nullptr) return PRCR_ERR_NULL;
-  const ChunkPlan plan = plan_chunk(p.capacity, batch, total_q, n_q_heads, n_kv_heads, rope->head_dim, dtype);
+  const ChunkPlan plan = plan_chunk(p.capacity, batch, total_q, n_q_heads, n_kv_heads, rope->head_dim);
+  if (plan.bytes > 0 && workspace == nullptr) return PRCR_ERR_NULL;
   if (workspace_bytes < plan.bytes) return PRCR_ERR_SHAPE;
   if (!aligned(out, 16) || !aligned(lse, 4)) return PRCR_ERR_ALIGN;
   const double row_bytes = static_cast<double>(rope->head_dim) * elem_bytes(dtype), rows = static_cast<double>(total_q) * n_q_heads;
@@ -191,9 +191,7 @@ prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,
   if (aliases(written, read)) return PRCR_ERR_ALIAS;
   p.out = out;
   p.lse = lse;
-  p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.rotated_bytes);
-  const prcr_status rotated = launch_status(launch_rotate(p, dtype, rope->head_dim, stream));
-  if (rotated != PRCR_OK) return rotated;
+  p.part = static_cast<float *>(workspace);
   return launch_status(launch_chunk(p, plan, dtype, rope->head_dim, cache->paged != 0, stream));
 }
 
@@ -222,7 +220,7 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache, prc
   const prcr_status st = prepare(rope, cache, dtype, batch, n_layers, n_kv_heads, layer, q, n_q_heads, q_off, q_len,
                                  total_q, q_pos, cache_len, scale, workspace, err_flag, &p);
   if (st != PRCR_OK) return st;
-  if (weights == nullptr || (total_q > 0 && lse == nullptr)) return PRCR_ERR_NULL;
+  if (weights == nullptr || (total_q > 0 && (lse == nullptr || workspace == nullptr))) return PRCR_ERR_NULL;
   if (window < 0) return PRCR_ERR_SHAPE;
   const double row_bytes = static_cast<double>(rope->head_dim) * elem_bytes(dtype), rows = static_cast<double>(total_q) * n_q_heads;
   const WeightsPlan plan = plan_key_weights(p.capacity, batch, total_q, n_q_heads, n_kv_heads, rope->head_dim, window, dtype);

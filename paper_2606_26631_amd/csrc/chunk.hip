@@ -13,6 +13,7 @@
 // each, and the weights are, in the registers where they arise, the operand of the value
 // product V^T x P^T, whose contraction may take the keys in any order.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "attend.h"
@@ -27,26 +28,41 @@ __device__ __forceinline__ void load_to_lds(const char *from, char *to) {
                                    (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
 
-// The sequence that tile slot `slot` belongs to: sequence b has the slots from
-// floor(q_off[b] G / M) + b on, enough of them for its rows' tiles of M.
+// The sequence that tile slot `slot` belongs to, and what the tile has to know of it.
+// Sequence b has the slots from floor(q_off[b] G / M) + b on, enough of them for its rows'
+// tiles of M.  Up to 64 sequences are one round of loads, a sequence per lane: every round costs
+// about a microsecond before the first key.
+struct Sequence {
+  int b, slot0;                              // and its first slot
+  Rows rows;
+  int32_t len;
+};
 template <int M>
-__device__ __forceinline__ int32_t first_slot(const AttendParams &p, int b) {
-  const uint32_t off = static_cast<uint32_t>(min(max(p.q_off[b], 0), p.total_q));
-  return static_cast<int32_t>(off * static_cast<uint32_t>(p.group) / M) + b;
+__device__ __forceinline__ int32_t first_slot(const AttendParams &p, int b, int32_t off) {
+  return static_cast<int32_t>(static_cast<uint32_t>(min(max(off, 0), p.total_q)) * static_cast<uint32_t>(p.group) / M) + b;
 }
 template <int M>
-__device__ __forceinline__ int sequence_of_slot(const AttendParams &p, int lane, int slot) {
+__device__ __forceinline__ Sequence sequence_of_slot(const AttendParams &p, int lane, int slot) {
   int lo = 0, n = p.batch;                   // among sequences lo .. lo + n - 1, the last that starts by `slot`
   while (n > kWave) {
     const int step = (n + kWave - 1) / kWave;
     const int b = lo + lane * step;
-    const bool ok = lane * step < n && first_slot<M>(p, b) <= slot;
+    const bool ok = lane * step < n && first_slot<M>(p, b, p.q_off[b]) <= slot;
     const int k = max(__popcll(__ballot(ok)) - 1, 0) * step;
     lo += k;
     n = min(step, n - k);
   }
-  const bool ok = lane < n && first_slot<M>(p, lo + lane) <= slot;
-  return __builtin_amdgcn_readfirstlane(lo + max(__popcll(__ballot(ok)) - 1, 0));
+  const int b = lo + min(lane, n - 1);
+  const Rows rows = rows_of(p, b);
+  const int32_t len = clamp_length(p.cache_len[b], p.capacity);
+  const int32_t slot0 = first_slot<M>(p, b, rows.start);
+  const int k = max(__popcll(__ballot(lane < n && slot0 <= slot)) - 1, 0);
+  Sequence s;
+  s.b = __builtin_amdgcn_readfirstlane(lo + k);
+  s.slot0 = __builtin_amdgcn_readlane(slot0, k);
+  s.rows = Rows{__builtin_amdgcn_readlane(rows.start, k), __builtin_amdgcn_readlane(rows.n, k), false};
+  s.len = __builtin_amdgcn_readlane(len, k);
+  return s;
 }
 
 // What a tile of the cache's rows in LDS looks like.  A row's 16-byte chunks are permuted
@@ -83,18 +99,23 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane & 31, half = lane / 32;
-  uint32_t id = blockIdx.x;
+  // The lane's rotary pair (one wave read of the arguments, in flight from the start).
+  const double freq = p.inv_freq[lane % (D / 2)];
+  const int axis = p.axis[lane % (D / 2)];
+  if (blockIdx.x == 0 && p.err != nullptr) report(p, threadIdx.x, kWaves * kWave);
+  const uint32_t id = blockIdx.x;
   const uint32_t by_head = p.by_heads.divide(id);
   const int kvh = static_cast<int>(id - by_head * static_cast<uint32_t>(p.n_kv_heads));
   const uint32_t by_split = p.by_split.divide(by_head);
   const int split = static_cast<int>(by_head - by_split * static_cast<uint32_t>(p.n_split));
   const int slot = p.n_slots - 1 - static_cast<int>(by_split);   // a prompt's last tiles see the most keys: first
-  const int b = sequence_of_slot<M>(p, lane, slot);
-  const Rows rows = rows_of(p, b);
-  const int32_t len = clamp_length(p.cache_len[b], p.capacity);
+  const Sequence seq = sequence_of_slot<M>(p, lane, slot);
+  const int b = seq.b;
+  const Rows rows = seq.rows;
+  const int32_t len = seq.len;
   const int G = p.group;
   const int n_rows = rows.n * G;
-  const int r0 = (slot - first_slot<M>(p, b)) * M;
+  const int r0 = (slot - seq.slot0) * M;
   if (r0 < 0 || r0 >= n_rows) return;
 
   const int first = len - rows.n;            // slot of the sequence's first row
@@ -113,15 +134,12 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   const int limit = first + token;
   const int wmax = __builtin_amdgcn_readlane(limit, 31);
 
-  // Query operand.  bf16: of product kk, elements 16 kk + 8 half + 0..7.  float32: the
-  // lane's half of the row, in order.
-  constexpr int kQ = kHalf ? D / 16 : D / 8;   // 16-byte chunks
+  constexpr int kQ = Tile::kChunks / 2;      // 16-byte chunks of the lane's half of a row: 2 i + half
   u32x4 q[kQ];
   {
-    const char *at = static_cast<const char *>(p.rotated) + row * kRowBytes;
+    const char *const at = static_cast<const char *>(p.q) + row * kRowBytes;
 #pragma unroll
-    for (int i = 0; i < kQ; ++i)
-      q[i] = *reinterpret_cast<const u32x4 *>(at + (kHalf ? 2 * i + half : half * kQ + i) * 16);
+    for (int i = 0; i < kQ; ++i) q[i] = load_nt(at + (2 * i + half) * 16);
   }
 
   // Rows of a tile: every load is issued for a row that exists; rows past the sequence's last
@@ -184,6 +202,50 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
     live_next = load_tile(t0, s_kv[t0 & 1]);
     if constexpr (kPaged) entry = entry_of(min(t0 + 1, t1 - 1), &entry_off);
   }
+
+  // The rows are turned while the first tile comes: in double precision, rounded once to the
+  // stored type, as prefill capture rotates the keys.  (The matrix products take operands
+  // of that type, so a query is rounded to it at some point; rounded here, the scores are those
+  // of two rows of the same kind, and their sums stay in float32.)  The wave's tokens' cosines
+  // and sines go through its share of the second tile's buffer, a few tokens at a time, since
+  // the rows of a group share them; a pair's place is permuted by the token, for the banks.
+  if (active && t0 < t1) {
+    constexpr int P = D / 2, kPer = Store<T>::kPerChunk;
+    constexpr int kTokens = 2 * Tile::kBytes / kWaves / (P * 16) < 32 ? 2 * Tile::kBytes / kWaves / (P * 16) : 32;
+    static_assert(kTokens >= 4 && (kTokens & (kTokens - 1)) == 0, "tokens of a pass");
+    typedef double f64x2 __attribute__((ext_vector_type(2)));
+    f64x2 *const table = reinterpret_cast<f64x2 *>(&s_kv[(t0 + 1) & 1][0][0] + wave * (2 * Tile::kBytes / kWaves));
+    const int tok0 = __builtin_amdgcn_readfirstlane(token), tok1 = __builtin_amdgcn_readlane(token, 31);
+    for (int c0 = tok0; c0 <= tok1; c0 += kTokens) {
+      const int n = min(kTokens, tok1 + 1 - c0);
+      for (int i = lane; i < n * P; i += kWave) {
+        const int tok = i / P, pair = i % P;                 // (of a lane, always the same pair)
+        const int32_t pos = p.q_pos[(static_cast<int64_t>(rows.start) + c0 + tok) * 3 + axis];
+        double sn, cs;
+        turn(static_cast<double>(pos) * freq, &sn, &cs);
+        table[tok * P + (pair ^ (tok & 7))] = p.negate ? f64x2{-cs, -sn} : f64x2{cs, sn};
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own writes)
+      const int tok = token - c0;
+      if (tok >= 0 && tok < n) {
+#pragma unroll
+        for (int i = 0; i < kQ / 2; ++i) {
+          double cs[kPer], sn[kPer];
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) {
+            const f64x2 x = table[tok * P + (((2 * i + half) * kPer + e) ^ (tok & 7))];
+            cs[e] = x[0];
+            sn[e] = x[1];
+          }
+          u32x4 lo, hi;
+          Store<T>::rotate(q[i], q[i + kQ / 2], cs, sn, lo, hi);
+          q[i] = lo;
+          q[i + kQ / 2] = hi;
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (its reads, before the next tokens)
+    }
+  }
   // One tile.  The first tiles, which every row sees whole, have neither the mask nor, between
   // their reads and products, what is done for it: kMasked is right for every tile.
   auto step = [&](int t, auto is_masked) {
@@ -216,7 +278,7 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
           s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
                                                           __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
         } else {
-          const f32x4 k = *reinterpret_cast<const f32x4 *>(krow + ((half * kQ + i) ^ sw) * 16);
+          const f32x4 k = *reinterpret_cast<const f32x4 *>(krow + ((2 * i + half) ^ sw) * 16);
           const f32x4 x = __builtin_bit_cast(f32x4, q[i]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], x[e], s[kb], 0, 0, 0);
@@ -404,19 +466,32 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
     }
 }
 
-// Merge of a row's partial results: a wave per row, D / 64 features a lane.  Splits without
-// keys have a sum of zero and no features.
+// Merge of a row's partial results: a wave per row, D / 64 features a lane.  The splits'
+// maxima and sums are read a split per lane, and the features of kPre splits at once with them:
+// one round of loads where there are no more.  Splits without keys have a sum of zero, and no
+// features.
 constexpr int kMergeWaves = 4;
+constexpr int kMostSplits = kWave;
+constexpr int kPre = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(kMergeWaves * kWave) void merge_kernel(const AttendParams p) {
   constexpr int F = D / kWave;
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kMergeWaves + threadIdx.x / kWave;
   if (row >= static_cast<int64_t>(p.total_q) * p.n_q_heads) return;
-  // Rows of no sequence have no partial results: their token lies behind the sequence's last.
-  const int32_t token = static_cast<int32_t>(row / p.n_q_heads);
+  const float *const part = p.part + row * p.n_split * (D + 2);
+  auto at = [&](int s) -> const float * { return part + min(s, p.n_split - 1) * (D + 2); };
+  const float m = at(lane)[D], l = lane < p.n_split ? at(lane)[D + 1] : 0.f;
+  float o[kPre][F];
+#pragma unroll
+  for (int k = 0; k < kPre; ++k)
+#pragma unroll
+    for (int f = 0; f < F; ++f) o[k][f] = at(k)[f * kWave + lane];
+  // Rows of no sequence have no partial results: the token lies behind its sequence's last row.
+  const int32_t token = static_cast<int32_t>(p.by_row.divide(static_cast<uint32_t>(row)));
   int lo = 0, n = p.batch;                   // the last sequence that starts at or before the token
-  while (n > 1) {
+  bool mine = false;
+  while (n > kWave) {
     const int step = (n + kWave - 1) / kWave;
     const int b = lo + lane * step;
     const bool ok = lane * step < n && p.q_off[b] <= token;
@@ -424,19 +499,30 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void merge_kernel(const Attend
     lo += k;
     n = min(step, n - k);
   }
-  const Rows rows = rows_of(p, lo);
-  if (token < rows.start || token >= rows.start + rows.n) return;
-  const float *const part = p.part + row * p.n_split * (D + 2);
-  float M = -FLT_MAX;
-  for (int s = 0; s < p.n_split; ++s) M = part[s * (D + 2) + D + 1] != 0.f ? fmaxf(M, part[s * (D + 2) + D]) : M;
-  float L = 0.f, O[F] = {};
-  for (int s = 0; s < p.n_split; ++s) {
-    const float ls = part[s * (D + 2) + D + 1];
-    if (ls == 0.f) continue;
-    const float w = exp2_hw(part[s * (D + 2) + D] - M);
-    L += ls * w;
+  if (lane < n) {
+    const Rows rows = rows_of(p, lo + lane);
+    mine = token >= rows.start && token < rows.start + rows.n;
+  }
+  if (!__any(mine)) return;
+  const float M = wave_max(l != 0.f ? m : -FLT_MAX);
+  const float w = l != 0.f ? exp2_hw(m - M) : 0.f;
+  const float L = wave_sum(l * w);
+  float O[F] = {};
+  for (int k0 = 0; k0 < p.n_split; k0 += kPre) {
+    if (k0 > 0) {
 #pragma unroll
-    for (int f = 0; f < F; ++f) O[f] = fmaf(part[s * (D + 2) + f * kWave + lane], w, O[f]);
+      for (int k = 0; k < kPre; ++k)
+#pragma unroll
+        for (int f = 0; f < F; ++f) o[k][f] = at(k0 + k)[f * kWave + lane];
+    }
+#pragma unroll
+    for (int k = 0; k < kPre; ++k) {
+      if (k0 + k >= p.n_split) break;
+      const float lk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l), k0 + k));
+      const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k0 + k));
+#pragma unroll
+      for (int f = 0; f < F; ++f) O[f] = lk != 0.f ? fmaf(o[k][f], wk, O[f]) : O[f];
+    }
   }
   if (lane == 0 && p.lse != nullptr)
     p.lse[row] = L != 0.f ? (M + __builtin_amdgcn_logf(L)) * 0.693147180559945309f : -__builtin_inff();
@@ -475,20 +561,22 @@ hipError_t chunk_dim(const AttendParams &p, const ChunkPlan &plan, int head_dim,
 }  // namespace
 
 ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
-                     int32_t head_dim, prcr_dtype dtype) {
+                     int32_t head_dim) {
   ChunkPlan plan{};
   const int64_t group = n_q_heads / n_kv_heads;
   const int64_t rows = static_cast<int64_t>(total_q) * group;
   plan.waves = rows <= int64_t{64} * batch ? 1 : 4;
   plan.n_slots = static_cast<int32_t>(rows / (32 * plan.waves)) + batch;
-  // Enough workgroups for two per compute unit, none of fewer than 256 keys at full capacity.
+  // A call of too few tiles for two workgroups per compute unit splits the keys, by what that
+  // costs: a workgroup takes about a microsecond for 64 keys, and every split writes and reads
+  // a partial result of 4 (D + 2) bytes per row and head, at some 4 MB a microsecond.  (The
+  // lengths are on the device: the capacity stands for them.)
   const int64_t have = static_cast<int64_t>(plan.n_slots) * n_kv_heads;
-  const int64_t want = (512 + have - 1) / have, most = (capacity + 255) / 256;
-  plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min(want, most)));
-  const int64_t elem = dtype == PRCR_F32 ? 4 : 2;
-  plan.rotated_bytes = (static_cast<size_t>(total_q) * n_q_heads * head_dim * elem + 255) / 256 * 256;
-  plan.bytes = plan.rotated_bytes;
-  if (plan.n_split > 1) plan.bytes += static_cast<size_t>(total_q) * n_q_heads * plan.n_split * (head_dim + 2) * 4;
+  const double tiles = static_cast<double>(capacity) / 64, rows_all = static_cast<double>(total_q) * n_q_heads;
+  const double best = std::sqrt(tiles * 4e6 / (rows_all * 8 * (head_dim + 2)));
+  const int64_t most = std::min<int64_t>({(512 + have - 1) / have, (capacity + 63) / 64, kMostSplits});
+  plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most, static_cast<int64_t>(best))));
+  if (plan.n_split > 1) plan.bytes = static_cast<size_t>(total_q) * n_q_heads * plan.n_split * (head_dim + 2) * 4;
   return plan;
 }
 
@@ -498,6 +586,7 @@ hipError_t launch_chunk(const AttendParams &in, const ChunkPlan &plan, prcr_dtyp
   p.n_slots = plan.n_slots;
   p.n_split = plan.n_split;
   p.by_split = Divisor::of(plan.n_split);
+  p.by_row = Divisor::of(p.n_q_heads);
   if (dtype == PRCR_F32)
     return paged ? chunk_dim<float, true>(p, plan, head_dim, stream) : chunk_dim<float, false>(p, plan, head_dim, stream);
   return paged ? chunk_dim<uint16_t, true>(p, plan, head_dim, stream)

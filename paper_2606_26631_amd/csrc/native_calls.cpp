@@ -602,7 +602,7 @@ PyObject *chunk_attention(Args a) {
   const prcr_dtype dtype = dtype_of(cache.k);
   const int32_t b = to_int32(cache.rows()), nl = to_int32(cache.n_layers()), h = to_int32(cache.n_kv_heads());
   size_t bytes = 0;
-  if (prcr_chunk_workspace_size(&cache.c, dtype, b, rows.total, rows.heads, h, to_int32(D), &bytes) != PRCR_OK)
+  if (prcr_chunk_workspace_size(&cache.c, b, rows.total, rows.heads, h, to_int32(D), &bytes) != PRCR_OK)
     throw Skip();
   Workspace ws(a[11], cache.device, bytes);
   const at::Tensor err = err_of(a[12], cache.device);

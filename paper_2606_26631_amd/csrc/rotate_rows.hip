@@ -1,6 +1,7 @@
-// Rotation of query rows, before chunk attention and before the keys' weights: every row is
+// Rotation of query rows, before the keys' weights are summed: every row that counts is
 // turned at its own (t, h, w) position in double precision and rounded once to the stored
-// type, as prefill capture rotates the keys.  The matrix products take operands of the
+// type, as prefill capture rotates the keys
+// (chunk attention, which reads a row only for its own tile, turns it there).  The matrix products take operands of the
 // stored type, so a query is rounded to it at some point; rounded here, the scores are
 // those of two rows of the same kind, and their sums stay in float32.
 //
@@ -24,21 +25,27 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParam
   constexpr int kPer = Store<T>::kPerChunk;
   constexpr int kChunks = P / kPer;          // of a half row
   constexpr int kRowBytes = D * static_cast<int>(sizeof(T)), kHalf = kRowBytes / 2;
-  if (blockIdx.x == 0 && p.err != nullptr) {
-    int bits = 0;
-    for (int b = threadIdx.x; b < p.batch; b += kThreads) {
-      if (rows_of(p, b).bad) bits |= PRCR_DERR_OFFSETS;
-      const int32_t len = p.cache_len[b];
-      if (len != clamp_length(len, p.capacity)) bits |= PRCR_DERR_CAPACITY;
-    }
-    if (bits != 0) atomicOr(p.err, bits);
-  }
+  if (blockIdx.x == 0 && p.err != nullptr) report(p, threadIdx.x, kThreads);
   const int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
   if (id >= n) return;
   const int c = static_cast<int>(id % kChunks);
+  double freq[kPer];
+  int axis[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    freq[e] = p.inv_freq[c * kPer + e];
+    axis[e] = p.axis[c * kPer + e];
+  }
   const uint32_t unit = static_cast<uint32_t>(id / kChunks);        // token and group of heads (below 2^31)
-  const uint32_t t = by_groups.divide(unit);
-  const int h0 = static_cast<int>(unit - t * static_cast<uint32_t>(n_groups)) * kHeads;
+  const uint32_t token = by_groups.divide(unit);
+  const int h0 = static_cast<int>(unit - token * static_cast<uint32_t>(n_groups)) * kHeads;
+  uint32_t t = token;
+  if (p.window > 0) {                        // the last `window` rows of each sequence
+    const int b = static_cast<int>(p.by_split.divide(token)), i = static_cast<int>(token) - b * p.window;
+    const Rows rows = rows_of(p, b);
+    if (i >= rows.n) return;
+    t = static_cast<uint32_t>(rows.start + rows.n - 1 - i);
+  }
   const int64_t at = (static_cast<int64_t>(t) * p.n_q_heads + h0) * kRowBytes + c * 16;
   const char *const in = static_cast<const char *>(p.q) + at;
   char *const out = static_cast<char *>(p.rotated) + at;
@@ -50,11 +57,14 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParam
     lo[h] = load_nt(row);
     hi[h] = load_nt(row + kHalf);
   }
+  int32_t pos[3];
+#pragma unroll
+  for (int a = 0; a < 3; ++a) pos[a] = p.q_pos[static_cast<int64_t>(t) * 3 + a];
   double cs[kPer], sn[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
-    const int pair = c * kPer + e;
-    sincos(static_cast<double>(p.q_pos[static_cast<int64_t>(t) * 3 + p.axis[pair]]) * p.inv_freq[pair], &sn[e], &cs[e]);
+    const int32_t at_axis = axis[e] == 0 ? pos[0] : axis[e] == 1 ? pos[1] : pos[2];
+    turn(static_cast<double>(at_axis) * freq[e], &sn[e], &cs[e]);
     if (p.negate) {
       cs[e] = -cs[e];
       sn[e] = -sn[e];
@@ -71,9 +81,14 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParam
 }
 
 template <typename T, int D>
-hipError_t rotate(const AttendParams &p, hipStream_t stream) {
+hipError_t rotate(const AttendParams &in, hipStream_t stream) {
+  AttendParams p = in;
   const int n_groups = (p.n_q_heads + kHeads - 1) / kHeads;
-  const int64_t n = static_cast<int64_t>(p.total_q) * n_groups * (D / 2 / Store<T>::kPerChunk);
+  // A window that covers more rows than there are is none.
+  if (static_cast<int64_t>(p.window) * p.batch >= p.total_q) p.window = 0;
+  if (p.window > 0) p.by_split = Divisor::of(p.window);
+  const int64_t tokens = p.window > 0 ? static_cast<int64_t>(p.window) * p.batch : p.total_q;
+  const int64_t n = tokens * n_groups * (D / 2 / Store<T>::kPerChunk);
   const int64_t blocks = (n + kThreads - 1) / kThreads;
   if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
   rotate_rows_kernel<T, D><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, Divisor::of(n_groups), n_groups, n);
