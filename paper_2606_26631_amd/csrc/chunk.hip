@@ -141,6 +141,19 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
 #pragma unroll
     for (int i = 0; i < kQ; ++i) q[i] = load_nt(at + (2 * i + half) * 16);
   }
+  // The wave's tokens, and the positions of the first kTokens of them on the lane's axis (with
+  // 32 pairs, of every second one), in flight before the tile is asked for.
+  constexpr int P = D / 2, kShare = kWave / P;
+  constexpr int kTokens = 2 * Tile::kBytes / kWaves / (P * 16) < 8 ? 2 * Tile::kBytes / kWaves / (P * 16) : 8;
+  static_assert(kTokens >= kShare && (kTokens & (kTokens - 1)) == 0, "tokens of a pass");
+  const int tok0 = __builtin_amdgcn_readfirstlane(token), tok1 = __builtin_amdgcn_readlane(token, 31);
+  int32_t pos[kTokens / kShare];
+  auto load_pos = [&](int c0) {
+#pragma unroll
+    for (int i = 0; i < kTokens / kShare; ++i)
+      pos[i] = p.q_pos[(static_cast<int64_t>(rows.start) + min(c0 + i * kShare + lane / P, tok1)) * 3 + axis];
+  };
+  load_pos(tok0);
 
   // Rows of a tile: every load is issued for a row that exists; rows past the sequence's last
   // one, or in a block outside the pool, are left out by the mask.
@@ -210,20 +223,19 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   // and sines go through its share of the second tile's buffer, a few tokens at a time, since
   // the rows of a group share them; a pair's place is permuted by the token, for the banks.
   if (active && t0 < t1) {
-    constexpr int P = D / 2, kPer = Store<T>::kPerChunk;
-    constexpr int kTokens = 2 * Tile::kBytes / kWaves / (P * 16) < 32 ? 2 * Tile::kBytes / kWaves / (P * 16) : 32;
-    static_assert(kTokens >= 4 && (kTokens & (kTokens - 1)) == 0, "tokens of a pass");
+    constexpr int kPer = Store<T>::kPerChunk;
     typedef double f64x2 __attribute__((ext_vector_type(2)));
     f64x2 *const table = reinterpret_cast<f64x2 *>(&s_kv[(t0 + 1) & 1][0][0] + wave * (2 * Tile::kBytes / kWaves));
-    const int tok0 = __builtin_amdgcn_readfirstlane(token), tok1 = __builtin_amdgcn_readlane(token, 31);
     for (int c0 = tok0; c0 <= tok1; c0 += kTokens) {
       const int n = min(kTokens, tok1 + 1 - c0);
-      for (int i = lane; i < n * P; i += kWave) {
-        const int tok = i / P, pair = i % P;                 // (of a lane, always the same pair)
-        const int32_t pos = p.q_pos[(static_cast<int64_t>(rows.start) + c0 + tok) * 3 + axis];
+      if (c0 != tok0) load_pos(c0);
+#pragma unroll
+      for (int i = 0; i < kTokens / kShare; ++i) {
+        const int tok = i * kShare + lane / P;
+        if (i * kShare >= n) break;          // (past the wave's last token: not read)
         double sn, cs;
-        turn(static_cast<double>(pos) * freq, &sn, &cs);
-        table[tok * P + (pair ^ (tok & 7))] = p.negate ? f64x2{-cs, -sn} : f64x2{cs, sn};
+        turn(static_cast<double>(pos[i]) * freq, &sn, &cs);
+        table[tok * P + (lane % P ^ (tok & 7))] = p.negate ? f64x2{-cs, -sn} : f64x2{cs, sn};
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own writes)
       const int tok = token - c0;
@@ -265,23 +277,31 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
 
     // Scores: lane's keys 32 kb + 8 (i / 4) + 4 half + i % 4 of row l32.
     f32x16 s[KB];
+    {
+      // All of the tile's key operands are on their way before the first product waits for one.
+      u32x4 k[KB][kQ];
+      const char *const krow = kt + l32 * kRowBytes;
+      const int sw = Tile::key_swizzle(l32);   // (32 rows on, the same)
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
-      const char *const krow = kt + (32 * kb + l32) * kRowBytes;
-      const int sw = Tile::key_swizzle(l32);   // (32 kb changes nothing in it)
+        for (int i = 0; i < kQ; ++i)
+          k[kb][i] = *reinterpret_cast<const u32x4 *>(krow + 32 * kb * kRowBytes + ((2 * i + half) ^ sw) * 16);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < kQ; ++i) {
-        if constexpr (kHalf) {
-          const u32x4 k = *reinterpret_cast<const u32x4 *>(krow + ((2 * i + half) ^ sw) * 16);
-          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
-                                                          __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
-        } else {
-          const f32x4 k = *reinterpret_cast<const f32x4 *>(krow + ((2 * i + half) ^ sw) * 16);
-          const f32x4 x = __builtin_bit_cast(f32x4, q[i]);
+      for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], x[e], s[kb], 0, 0, 0);
+        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          if constexpr (kHalf) {
+            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[kb][i]),
+                                                            __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
+          } else {
+            const f32x4 a = __builtin_bit_cast(f32x4, k[kb][i]), x = __builtin_bit_cast(f32x4, q[i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], x[e], s[kb], 0, 0, 0);
+          }
         }
       }
     }
