@@ -224,6 +224,7 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   // the rows of a group share them; a pair's place is permuted by the token, for the banks.
   if (active && t0 < t1) {
     constexpr int kPer = Store<T>::kPerChunk;
+    // A pair's cosine and sine, 16 bytes: doubles, or (bf16) as two floats each.
     typedef double f64x2 __attribute__((ext_vector_type(2)));
     f64x2 *const table = reinterpret_cast<f64x2 *>(&s_kv[(t0 + 1) & 1][0][0] + wave * (2 * Tile::kBytes / kWaves));
     for (int c0 = tok0; c0 <= tok1; c0 += kTokens) {
@@ -235,24 +236,43 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
         if (i * kShare >= n) break;          // (past the wave's last token: not read)
         double sn, cs;
         turn(static_cast<double>(pos[i]) * freq, &sn, &cs);
-        table[tok * P + (lane % P ^ (tok & 7))] = p.negate ? f64x2{-cs, -sn} : f64x2{cs, sn};
+        if (p.negate) {
+          cs = -cs;
+          sn = -sn;
+        }
+        f64x2 both = {cs, sn};
+        if constexpr (kHalf) {
+          const float c = static_cast<float>(cs), s = static_cast<float>(sn);
+          both = __builtin_bit_cast(f64x2, f32x4{c, static_cast<float>(cs - static_cast<double>(c)), s,
+                                                 static_cast<float>(sn - static_cast<double>(s))});
+        }
+        table[tok * P + (lane % P ^ (tok & 7))] = both;
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own writes)
       const int tok = token - c0;
       if (tok >= 0 && tok < n) {
 #pragma unroll
         for (int i = 0; i < kQ / 2; ++i) {
-          double cs[kPer], sn[kPer];
+          f64x2 angle[kPer];
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) {
-            const f64x2 x = table[tok * P + (((2 * i + half) * kPer + e) ^ (tok & 7))];
-            cs[e] = x[0];
-            sn[e] = x[1];
+          for (int e = 0; e < kPer; ++e) angle[e] = table[tok * P + (((2 * i + half) * kPer + e) ^ (tok & 7))];
+          if constexpr (kHalf) {
+            f32x4 split[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) split[e] = __builtin_bit_cast(f32x4, angle[e]);
+            turn_bf16(q[i], q[i + kQ / 2], split);
+          } else {
+            double cs[kPer], sn[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+              cs[e] = angle[e][0];
+              sn[e] = angle[e][1];
+            }
+            u32x4 lo, hi;
+            Store<T>::rotate(q[i], q[i + kQ / 2], cs, sn, lo, hi);
+            q[i] = lo;
+            q[i + kQ / 2] = hi;
           }
-          u32x4 lo, hi;
-          Store<T>::rotate(q[i], q[i + kQ / 2], cs, sn, lo, hi);
-          q[i] = lo;
-          q[i + kQ / 2] = hi;
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (its reads, before the next tokens)
