@@ -470,7 +470,7 @@ prcr_status prcr_key_weights_workspace_size(const prcr_cache *cache, prcr_dtype 
  *                  (a revisit of that token then raises PRCR_DERR_INDEX and skips it).  Only
  *                  v, v_slot, batch and max_visual of it are read.  Such memories must
  *                  be given: their slots are wrong after the call otherwise.
- *   workspace      prcr_evict_workspace_size() bytes
+ *   workspace      prcr_evict_workspace_size() bytes, 8-byte aligned
  * Rows of slots from new_cache_len[b] on are left as they are.  Paged: the block table stays; blocks
  * past the new length are the caller's to reuse, and a sequence's blocks must not be
  * another one's too.  A block-table entry outside the pool skips its rows (PRCR_DERR_BLOCK).
@@ -484,8 +484,9 @@ prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
                        void *workspace, size_t workspace_bytes, int32_t *err_flag,
                        hipStream_t stream);
 
-/* Workspace bytes prcr_evict needs (host). */
-prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch, size_t *bytes);
+/* Workspace bytes prcr_evict needs for this cache and budget (host). */
+prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch,
+                                      int32_t budget, size_t *bytes);
 
 /* Host helpers (no GPU work). */
 

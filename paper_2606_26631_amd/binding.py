@@ -127,7 +127,7 @@ def lib() -> ctypes.CDLL:
                                    c_void_p, c_void_p, c_void_p, c_int32, ctypes.c_float, c_int32,
                                    c_void_p, c_void_p, ctypes.c_size_t, c_void_p, c_void_p]
     L.prcr_evict_workspace_size.restype = c_int
-    L.prcr_evict_workspace_size.argtypes = [POINTER(CCache), c_int32, POINTER(ctypes.c_size_t)]
+    L.prcr_evict_workspace_size.argtypes = [POINTER(CCache), c_int32, c_int32, POINTER(ctypes.c_size_t)]
     L.prcr_evict.restype = c_int
     L.prcr_evict.argtypes = [POINTER(CCache), c_int, c_int32, c_int32, c_int32, c_int32, c_void_p,
                              c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
@@ -785,9 +785,9 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
     return weights
 
 
-def evict_workspace_bytes(cache: Cache) -> int:
+def evict_workspace_bytes(cache: Cache, budget: int) -> int:
     """Bytes of workspace prcr_evict needs (prcr_evict_workspace_size)."""
-    return _size_t("prcr_evict_workspace_size", ctypes.byref(cache.to_c()), _batch(cache))
+    return _size_t("prcr_evict_workspace_size", ctypes.byref(cache.to_c()), _batch(cache), int(budget))
 
 
 def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, keep_last: int = 0, mem=None,
@@ -825,7 +825,7 @@ def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, ke
     _shape(kept, "kept", (B, budget))
     _need(new_weights, "new_weights", torch.float32, 3, cache.device)
     _shape(new_weights, "new_weights", (B, H, cap))
-    workspace = _workspace(workspace, evict_workspace_bytes(cache), cache.device, stream)
+    workspace = _workspace(workspace, evict_workspace_bytes(cache, budget), cache.device, stream)
     _err(err, cache.device)
     st = lib().prcr_evict(
         ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H), int(D), _ptr(cache_len),

@@ -59,7 +59,9 @@ struct EvictParams {
   int32_t *kept;                  // [batch][budget]
   float *new_weights;             // [batch][n_kv_heads][capacity] or null
   int32_t *v_slot;                // [batch][max_visual] of a key-only memory, or null
-  float *score;                   // workspace [batch][capacity]
+  float *score;                   // workspace [batch][capacity]: the scores' order as integers
+  int32_t *first_moved;           // workspace [batch]: the first kept slot that moves
+  uint32_t __attribute__((ext_vector_type(2))) *moves;   // workspace, paged: [batch][budget] pool slots, from and to
   int32_t *err;
   int32_t batch, n_layers, n_kv_heads, row_bytes;
   int32_t s_max, block_size, max_blocks, n_blocks, capacity;
@@ -180,8 +182,14 @@ __device__ __forceinline__ void turn(double x, double *sn, double *cs) {
   *cs = (q + 1) & 2 ? -b : b;
 }
 
-// One pair of 16-byte chunks of bf16 rows, turned and rounded once to bf16.  cs and sn hold a
-// pair's cosine and sine as two floats each, (high, low), exact to 2^-49.  In float32 with the
+// A cosine and a sine as two floats each: cos high, cos low, sin high, sin low.
+__device__ __forceinline__ f32x4 split_angle(double cs, double sn) {
+  const float c = static_cast<float>(cs), s = static_cast<float>(sn);
+  return f32x4{c, static_cast<float>(cs - static_cast<double>(c)), s, static_cast<float>(sn - static_cast<double>(s))};
+}
+
+// One pair of 16-byte chunks of bf16 rows, turned and rounded once to bf16.  The
+// angles are split as above, exact to 2^-49.  In float32 with the
 // products' errors kept, the result is within one unit of float32 of the exact one, so its
 // rounding to bf16 is that of the exact one unless it lies that near to the middle of two bf16
 // numbers; a chunk with such an element (some lane's, in one of ten) is done again in double.

@@ -246,13 +246,16 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache, prc
   return launch_status(launch_key_weights(p, plan, dtype, rope->head_dim, cache->paged != 0, stream));
 }
 
-prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch, size_t *bytes) {
+prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch, int32_t budget, size_t *bytes) {
   if (bytes == nullptr) return PRCR_ERR_NULL;
   int64_t capacity = 0;
   prcr_status st = check_heads(batch, 1, 64);
   if (st == PRCR_OK) st = cache_shape(cache, &capacity);
+  if (st == PRCR_OK && budget < 1) st = PRCR_ERR_SHAPE;
   if (st != PRCR_OK) return st;
-  *bytes = static_cast<size_t>(batch) * (static_cast<size_t>(capacity) + 1) * 4;
+  // Paged: a kept slot's two places; then the scores; then the first slots that move.
+  *bytes = static_cast<size_t>(batch) * ((cache->paged ? static_cast<size_t>(budget) * 8 : 0) +
+                                         (static_cast<size_t>(capacity) + 1) * 4);
   return PRCR_OK;
 }
 
@@ -272,7 +275,7 @@ prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
       static_cast<int64_t>(keep_first) + keep_last > budget)
     return PRCR_ERR_SHAPE;
   size_t need = 0;
-  if ((st = prcr_evict_workspace_size(cache, batch, &need)) != PRCR_OK) return st;
+  if ((st = prcr_evict_workspace_size(cache, batch, budget, &need)) != PRCR_OK) return st;
   if (workspace_bytes < need) return PRCR_ERR_SHAPE;
   // Only a key-only memory names cache slots.
   const bool rename = mem != nullptr && mem->v == nullptr;
@@ -282,7 +285,7 @@ prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
     if (!aligned(mem->v_slot, 4)) return PRCR_ERR_ALIGN;
   }
   if (!aligned(cache_len, 4) || !aligned(weights, 4) || !aligned(new_cache_len, 4) || !aligned(kept, 4) ||
-      !aligned(new_weights, 4) || !aligned(workspace, 4) || !aligned(err_flag, 4))
+      !aligned(new_weights, 4) || !aligned(workspace, 8) || !aligned(err_flag, 4))
     return PRCR_ERR_ALIGN;
   const double all = cache_bytes(*cache, batch, n_layers, n_kv_heads, static_cast<double>(head_dim) * elem_bytes(dtype));
   const double w = 4.0 * batch * n_kv_heads * static_cast<double>(capacity), nb4 = batch * 4.0;
@@ -303,7 +306,10 @@ prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
   p.kept = kept;
   p.new_weights = new_weights;
   p.v_slot = rename ? mem->v_slot : nullptr;
-  p.score = static_cast<float *>(workspace);
+  char *const scores = static_cast<char *>(workspace) + (cache->paged ? static_cast<size_t>(batch) * budget * 8 : 0);
+  p.moves = cache->paged ? static_cast<decltype(p.moves)>(workspace) : nullptr;
+  p.score = reinterpret_cast<float *>(scores);
+  p.first_moved = reinterpret_cast<int32_t *>(p.score + static_cast<int64_t>(batch) * capacity);
   p.err = err_flag;
   p.batch = batch;
   p.n_layers = n_layers;

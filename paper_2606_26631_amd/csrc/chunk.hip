@@ -241,11 +241,7 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
           sn = -sn;
         }
         f64x2 both = {cs, sn};
-        if constexpr (kHalf) {
-          const float c = static_cast<float>(cs), s = static_cast<float>(sn);
-          both = __builtin_bit_cast(f64x2, f32x4{c, static_cast<float>(cs - static_cast<double>(c)), s,
-                                                 static_cast<float>(sn - static_cast<double>(s))});
-        }
+        if constexpr (kHalf) both = __builtin_bit_cast(f64x2, split_angle(cs, sn));
         table[tok * P + (lane % P ^ (tok & 7))] = both;
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own writes)

@@ -21,7 +21,8 @@ namespace {
 constexpr int kSelect = 1024;                // threads of kernel 1
 constexpr int kSelectWaves = kSelect / kWave;
 constexpr int kMove = 256;                   // threads of kernel 2
-constexpr int kDeep = 8;                     // rows a thread has in flight
+constexpr int kDeep = 4;                     // rows of a batch that a thread has a chunk of
+constexpr uint32_t kNowhere = ~0u;           // (a pool's slots are at least 128 bytes each: never so many)
 
 // Order of scores as unsigned integers.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -41,8 +42,9 @@ __global__ __launch_bounds__(kSelect) void select_kernel(const EvictParams p) {
   const int n = clamp_length(len, p.capacity);
   int32_t *const kept = p.kept + static_cast<int64_t>(b) * p.budget;
   const int n_new = min(n, p.budget);
-  // The slots that stay in place at the front, for kernel 2 (after the scores).
-  int32_t *const first_moved = reinterpret_cast<int32_t *>(p.score + static_cast<int64_t>(p.batch) * p.capacity) + b;
+  // For kernel 2: the kept slots that stay in place at the front; paged, where the others come
+  // from and go to.
+  int32_t *const first_moved = p.first_moved + b;
   if (len != n && tid == 0 && p.err != nullptr) atomicOr(p.err, PRCR_DERR_CAPACITY);
   __syncthreads();                           // (new_len may be cache_len)
   if (tid == 0) p.new_len[b] = n_new;
@@ -133,10 +135,25 @@ __global__ __launch_bounds__(kSelect) void select_kernel(const EvictParams p) {
   for (int d = 1; d < kWave; d <<= 1) moved = min(moved, __shfl_xor(moved, d));
   if (lane == 0) s_more[wave] = static_cast<uint32_t>(moved);
   __syncthreads();
-  if (tid == 0) {
-    for (int v = 1; v < kSelectWaves; ++v) moved = min(moved, static_cast<int>(s_more[v]));
-    *first_moved = moved;
+  for (int v = 0; v < kSelectWaves; ++v) moved = min(moved, static_cast<int>(s_more[v]));
+  if (tid == 0) *first_moved = moved;
+  if (p.moves == nullptr) return;
+  // (The barriers above order the list's writes before these reads of it.)
+  bool bad = false;
+  auto in_pool = [&](int slot) -> uint32_t {
+    const int lb = slot / p.block_size;
+    const int32_t blk = p.block_table[static_cast<int64_t>(b) * p.max_blocks + lb];
+    const bool ok = blk >= 0 && blk < p.n_blocks;
+    bad |= !ok;
+    return ok ? static_cast<uint32_t>(blk) * static_cast<uint32_t>(p.block_size) +
+                    static_cast<uint32_t>(slot - lb * p.block_size) : kNowhere;
+  };
+  for (int i = moved + tid; i < p.budget; i += kSelect) {
+    const uint32_t from = in_pool(kept[i]), to = in_pool(i);
+    p.moves[static_cast<int64_t>(b) * p.budget + i] = from == kNowhere || to == kNowhere ? u32x2{kNowhere, kNowhere}
+                                                                                         : u32x2{from, to};
   }
+  if (bad && p.err != nullptr) atomicOr(p.err, PRCR_DERR_BLOCK);
 }
 
 template <bool kPaged>
@@ -178,52 +195,59 @@ __global__ __launch_bounds__(kMove) void move_kernel(const EvictParams p, const 
   const int layer = static_cast<int>(by_head - by_layer * static_cast<uint32_t>(p.n_layers));
   const uint32_t operand = by_batch.divide(by_layer);
   const int b = static_cast<int>(by_layer - operand * static_cast<uint32_t>(p.batch));
-  char *const cache = static_cast<char *>(operand != 0 ? p.cache_v : p.cache_k);
+  const int n = p.new_len[b], i0 = p.first_moved[b];
+  if (i0 >= n) return;
+  const int chunks = p.row_bytes / 16;       // a power of two, at most 32
+  const int r = tid / chunks, step = kMove / chunks;
+  // Slot 0's row of this layer (paged: the pool's) and head, and the bytes from a slot to the next.
+  const int64_t base = kPaged ? static_cast<int64_t>(layer) * p.n_blocks * p.block_size * p.n_kv_heads + kvh
+                              : ((static_cast<int64_t>(b) * p.n_layers + layer) * p.n_kv_heads + kvh) * p.s_max;
+  char *const rows = static_cast<char *>(operand != 0 ? p.cache_v : p.cache_k) + base * p.row_bytes +
+                     (tid & (chunks - 1)) * 16;
+  const uint64_t slot_bytes = static_cast<uint64_t>(p.row_bytes) * (kPaged ? p.n_kv_heads : 1);
   const int32_t *const kept = p.kept + static_cast<int64_t>(b) * p.budget;
-  const int n = p.new_len[b];
-  const int i0 = reinterpret_cast<const int32_t *>(p.score + static_cast<int64_t>(p.batch) * p.capacity)[b];
-  const int chunks = p.row_bytes / 16;       // a power of two, at most kMove
-  const int c = tid & (chunks - 1), r = tid / chunks, step = kMove / chunks;
-  const int32_t *const table = kPaged ? p.block_table + static_cast<int64_t>(b) * p.max_blocks : nullptr;
-  bool bad = false;
-  // Chunk c of a slot's row; null in a block outside the pool.
-  auto row = [&](int slot) -> char * {
-    int64_t at;
-    if constexpr (kPaged) {
-      const int lb = slot / p.block_size;
-      const int32_t blk = table[lb];
-      if (blk < 0 || blk >= p.n_blocks) {
-        bad = true;
-        return nullptr;
-      }
-      at = ((static_cast<int64_t>(layer) * p.n_blocks + blk) * p.block_size + (slot - lb * p.block_size)) * p.n_kv_heads + kvh;
-    } else {
-      at = ((static_cast<int64_t>(b) * p.n_layers + layer) * p.n_kv_heads + kvh) * p.s_max + slot;
-    }
-    return cache + at * p.row_bytes + c * 16;
-  };
-  for (int i = i0; i < n; i += step * kDeep) {
+  const u32x2 *const moves = kPaged ? p.moves + static_cast<int64_t>(b) * p.budget : nullptr;
+  struct Batch {
     u32x4 x[kDeep];
-    char *to[kDeep];
+    u32x2 slots[kDeep];                      // from, to
+  };
+  auto look_up = [&](int first, Batch &d) {
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
-      const int at = i + u * step + r;
-      to[u] = nullptr;
-      if (at < n) {
-        const char *const from = row(kept[at]);
-        to[u] = row(at);
-        if (from == nullptr) to[u] = nullptr;
-        if (to[u] != nullptr) x[u] = *reinterpret_cast<const u32x4 *>(from);
-      }
+      const int i = first + u * step + r;
+      d.slots[u] = u32x2{kNowhere, kNowhere};
+      if (i < n) d.slots[u] = kPaged ? moves[i] : u32x2{static_cast<uint32_t>(kept[i]), static_cast<uint32_t>(i)};
     }
-    // Every row of the batch is in registers before one of it is written.
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  };
+  auto load = [&](Batch &d) {
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u)
+      if (d.slots[u][0] != kNowhere) d.x[u] = load_nt(rows + d.slots[u][0] * slot_bytes);
+  };
+  auto store = [&](Batch &d) {
+    // Every thread's share of the batch is in registers before one of it is written.
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u) asm volatile("" : "+v"(d.x[u]));
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kDeep; ++u)
-      if (to[u] != nullptr) *reinterpret_cast<u32x4 *>(to[u]) = x[u];
+      if (d.slots[u][1] != kNowhere) store_nt(rows + d.slots[u][1] * slot_bytes, d.x[u]);
+  };
+  // The next batch is on its way while one is written: it reads slots from its own first row
+  // on, which lie behind all that is written before it.
+  const int batch = kDeep * step;
+  Batch one, two;
+  look_up(i0, one);
+  load(one);
+  look_up(i0 + batch, two);
+  for (int i = i0; i < n; i += 2 * batch) {
+    load(two);
+    store(one);
+    look_up(i + 2 * batch, one);
+    load(one);
+    store(two);
+    look_up(i + 3 * batch, two);
   }
-  if (bad && p.err != nullptr) atomicOr(p.err, PRCR_DERR_BLOCK);
 }
 
 }  // namespace

@@ -286,7 +286,7 @@ WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, i
   int64_t tokens = (static_cast<int64_t>(total_q) + batch - 1) / batch;
   if (window > 0) tokens = std::min<int64_t>(tokens, window);
   const int64_t rows = tokens * (n_q_heads / n_kv_heads);     // of a sequence and KV head, on average
-  plan.blocks = dtype == PRCR_BF16 && rows > 64 ? 2 : 1;
+  plan.blocks = dtype == PRCR_BF16 && rows > 512 ? 2 : 1;
   const int64_t keys = kWaves * 32 * plan.blocks;
   plan.n_stretches = static_cast<int32_t>((capacity + keys - 1) / keys);
   const int64_t have = static_cast<int64_t>(plan.n_stretches) * batch * n_kv_heads;

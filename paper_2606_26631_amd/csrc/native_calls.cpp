@@ -681,7 +681,7 @@ PyObject *evict(Args a) {
   const prcr_dtype dtype = dtype_of(cache.k);
   const int32_t b = to_int32(B), nl = to_int32(cache.n_layers()), h = to_int32(H);
   size_t bytes = 0;
-  if (budget < 1 || prcr_evict_workspace_size(&cache.c, b, &bytes) != PRCR_OK) throw Skip();
+  if (budget < 1 || prcr_evict_workspace_size(&cache.c, b, budget, &bytes) != PRCR_OK) throw Skip();
   Workspace ws(a[10], cache.device, bytes);
   const at::Tensor err = err_of(a[11], cache.device);
   const Launch on(a[12], cache.device);

@@ -6,8 +6,9 @@
 // those of two rows of the same kind, and their sums stay in float32.
 //
 // A thread takes 16 bytes of each half of a token's rows: their angles' cosines and sines
-// once, then the rows of up to kHeads heads, all read before the first is turned.  What
-// bounds it is reading and writing the rows.  The first workgroup also reports what is wrong
+// once, then the rows of kHeads heads, all read before the first is turned.  What bounds it
+// is reading and writing the rows; of few rows, a thread's own work, and a thread has one head
+// then (32 tokens of 32 heads: 9.1 us with eight heads a thread).  The first workgroup also reports what is wrong
 // with the offsets and lengths, which the kernels after it only skip.
 #include "attend.h"
 #include "rotary.h"
@@ -15,10 +16,9 @@
 namespace prcr {
 namespace {
 
-constexpr int kHeads = 8;
 constexpr int kThreads = 64;
 
-template <typename T, int D>
+template <typename T, int D, int kHeads>
 __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParams p, const Divisor by_groups,
                                                                const int n_groups, const int64_t n) {
   constexpr int P = D / 2;
@@ -61,6 +61,7 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParam
 #pragma unroll
   for (int a = 0; a < 3; ++a) pos[a] = p.q_pos[static_cast<int64_t>(t) * 3 + a];
   double cs[kPer], sn[kPer];
+  f32x4 split[8];                            // (bf16: kPer is 8)
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const int32_t at_axis = axis[e] == 0 ? pos[0] : axis[e] == 1 ? pos[1] : pos[2];
@@ -69,18 +70,22 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParam
       cs[e] = -cs[e];
       sn[e] = -sn[e];
     }
+    if constexpr (sizeof(T) == 2) split[e] = split_angle(cs[e], sn[e]);
   }
 #pragma unroll
   for (int h = 0; h < kHeads; ++h) {
     if (h >= heads) break;
-    u32x4 a, b;
-    Store<T>::rotate(lo[h], hi[h], cs, sn, a, b);
+    u32x4 a = lo[h], b = hi[h];
+    if constexpr (sizeof(T) == 2)
+      turn_bf16(a, b, split);
+    else
+      Store<T>::rotate(lo[h], hi[h], cs, sn, a, b);
     *reinterpret_cast<u32x4 *>(out + h * kRowBytes) = a;
     *reinterpret_cast<u32x4 *>(out + h * kRowBytes + kHalf) = b;
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int kHeads>
 hipError_t rotate(const AttendParams &in, hipStream_t stream) {
   AttendParams p = in;
   const int n_groups = (p.n_q_heads + kHeads - 1) / kHeads;
@@ -91,15 +96,22 @@ hipError_t rotate(const AttendParams &in, hipStream_t stream) {
   const int64_t n = tokens * n_groups * (D / 2 / Store<T>::kPerChunk);
   const int64_t blocks = (n + kThreads - 1) / kThreads;
   if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
-  rotate_rows_kernel<T, D><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, Divisor::of(n_groups), n_groups, n);
+  rotate_rows_kernel<T, D, kHeads><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, Divisor::of(n_groups), n_groups, n);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t rotate_dim(const AttendParams &p, int head_dim, hipStream_t stream) {
+  // With a head a thread, fewer than 2^16 threads would be less than a wave on every SIMD.
+  if (static_cast<int64_t>(p.total_q) * p.n_q_heads * (head_dim / 16) < (1 << 19))
+    return head_dim == 64 ? rotate<T, 64, 1>(p, stream) : rotate<T, 128, 1>(p, stream);
+  return head_dim == 64 ? rotate<T, 64, 4>(p, stream) : rotate<T, 128, 4>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_rotate(const AttendParams &p, prcr_dtype dtype, int head_dim, hipStream_t stream) {
-  if (dtype == PRCR_F32) return head_dim == 64 ? rotate<float, 64>(p, stream) : rotate<float, 128>(p, stream);
-  return head_dim == 64 ? rotate<uint16_t, 64>(p, stream) : rotate<uint16_t, 128>(p, stream);
+  return dtype == PRCR_F32 ? rotate_dim<float>(p, head_dim, stream) : rotate_dim<uint16_t>(p, head_dim, stream);
 }
 
 }  // namespace prcr
