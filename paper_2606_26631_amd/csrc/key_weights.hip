@@ -5,7 +5,7 @@
 //
 // A workgroup takes a stretch of keys of one sequence and KV head, 32 kBlocks keys a wave, in
 // registers, and runs through the rows that see them, a tile at a time, which all its waves
-// read from LDS (two tiles of them, the next one's loads in flight).  The scores are formed as
+// read from LDS, the next tile's loads in flight.  The scores are formed as
 // Q (32 rows) x K^T (32 keys), so that a lane holds 16 rows' scores of one key and adds
 // their weights in its own registers: no other lane's, no atomics, a fixed order.  Where
 // that makes few workgroups, the rows are shared out over several, whose sums a second
@@ -41,7 +41,11 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
   constexpr int kBytes = kRows * kRowBytes;
   constexpr int kKeyBytes = kWaves * 32 * kRowBytes;
   static_assert(kMine >= 1, "a row tile is at least a load per wave");
-  __shared__ __align__(1024) char s_rows[2 * kBytes > kKeyBytes ? 2 * kBytes : kKeyBytes];
+  // Three tiles of rows.  The keys pass through there too: bf16, through the places of the
+  // second and third tile while the first one comes; float32, whose keys take more, before it.
+  constexpr bool kEarly = kHalf;
+  constexpr int kKeysAt = kEarly ? kBytes : 0;
+  __shared__ __align__(1024) char s_rows[3 * kBytes > kKeysAt + kKeyBytes ? 3 * kBytes : kKeysAt + kKeyBytes];
   __shared__ __align__(16) float s_lse[2][kRows];
   __shared__ __align__(16) int s_limit[2][kRows];
 
@@ -59,7 +63,7 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
   const int64_t head = static_cast<int64_t>(b) * p.n_kv_heads + kvh;
   float *const weights = p.weights + head * p.capacity;
   if (k0 >= len) {
-    if (!p.accumulate && part == 0)
+    if (!p.accumulate && p.n_split == 1)
       for (int j = k0 + threadIdx.x; j < min(k0 + kKeys, p.capacity); j += kThreads) weights[j] = 0.f;
     return;
   }
@@ -71,52 +75,8 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
   const int per = ((all1 - all0 + kRows - 1) / kRows + p.n_split - 1) / p.n_split * kRows;
   const int row0 = min(all0 + part * per, all1), n_rows = min(row0 + per, all1);
 
-  // The wave's keys, whole rows through LDS (in the operand's layout a load would read
-  // half of each of 32 rows' cache lines).  bf16: of product i, elements 16 i + 8 half + 0..7;
-  // float32: the lane's half of the row.
-  const int kw = k0 + wave * 32 * kBlocks;
   const int in_load = lane / kChunks, chunk = lane % kChunks;
   const int sw = l32 & (kChunks - 1);
-  u32x4 k[kBlocks][kQ];
-  bool live[kBlocks];
-  bool bad_block = false;
-#pragma unroll
-  for (int kb = 0; kb < kBlocks; ++kb) {
-    const int mine = kw + 32 * kb + l32;
-    const int j = min(mine, len - 1);
-    live[kb] = mine < len;
-    uint32_t slot = static_cast<uint32_t>(j);
-    if constexpr (kPaged) {
-      const int lb = p.block_shift >= 0 ? j >> p.block_shift : j / p.block_size;
-      const int32_t blk = p.block_table[static_cast<int64_t>(b) * p.max_blocks + lb];
-      const bool ok = blk >= 0 && blk < p.n_blocks;
-      bad_block |= live[kb] && !ok;
-      live[kb] = live[kb] && ok;
-      // (A pool's slots are at least 128 bytes each: below 2^32 of them.)
-      slot = ok ? static_cast<uint32_t>(blk) * static_cast<uint32_t>(p.block_size) +
-                      static_cast<uint32_t>(j - lb * p.block_size) : 0u;
-    }
-    const int64_t base = kPaged ? static_cast<int64_t>(p.layer) * p.n_blocks * p.block_size * p.n_kv_heads + kvh
-                                : ((static_cast<int64_t>(b) * p.n_layers + p.layer) * p.n_kv_heads + kvh) * p.s_max;
-    const uint32_t step = kPaged ? static_cast<uint32_t>(p.n_kv_heads) : 1u;
-    char *const to = s_rows + wave * 32 * kRowBytes;
-#pragma unroll
-    for (int i = 0; i < 32 / kRowsPerLoad; ++i) {
-      const int at = i * kRowsPerLoad + in_load;
-      const uint32_t row = static_cast<uint32_t>(__shfl(static_cast<int>(slot), at));
-      load_to_lds(static_cast<const char *>(p.cache_k) +
-                      (base + static_cast<int64_t>(static_cast<uint64_t>(row) * step)) * kRowBytes +
-                      (chunk ^ (at & (kChunks - 1))) * 16, to + i * 1024);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (a wave reads only what it loaded)
-#pragma unroll
-    for (int i = 0; i < kQ; ++i)
-      k[kb][i] = *reinterpret_cast<const u32x4 *>(to + l32 * kRowBytes + ((kHalf ? 2 * i + half : half * kQ + i) ^ sw) * 16);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (before the next rows, or the tiles, come there)
-  }
-  if (kPaged && p.err != nullptr && __any(bad_block) && lane == 0) atomicOr(p.err, PRCR_DERR_BLOCK);
-  __syncthreads();
-
   auto token_of = [&](int r) -> int { return static_cast<int>(p.by_group.divide(static_cast<uint32_t>(r))); };
   auto row_index = [&](int r, int token) -> int64_t {
     return (static_cast<int64_t>(rows.start) + token) * p.n_q_heads + kvh * G + (r - token * G);
@@ -143,28 +103,75 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
     if (r0 + static_cast<int>(threadIdx.x) >= n_rows || limit < 0) lse = __builtin_inff();
   };
 
-  double w[kBlocks] = {};                    // (the first keys add up every row there is: float32 lost 1e-6 of 10,000)
-  int buf = 0;
   if (row0 < n_rows) {
-    load_rows(row0, s_rows);
-    if (threadIdx.x < kRows) {
-      load_lse(row0);
-      s_lse[0][threadIdx.x] = lse;
-      s_limit[0][threadIdx.x] = limit;
+    if (threadIdx.x < kRows) load_lse(row0);
+    if (kEarly) load_rows(row0, s_rows);
+  }
+
+  // The wave's keys, whole rows through LDS (in the operand's layout a load would read
+  // half of each of 32 rows' cache lines).  bf16: of product i, elements 16 i + 8 half + 0..7;
+  // float32: the lane's half of the row.
+  const int kw = k0 + wave * 32 * kBlocks;
+  u32x4 k[kBlocks][kQ];
+  bool live[kBlocks];
+  bool bad_block = false;
+#pragma unroll
+  for (int kb = 0; kb < kBlocks; ++kb) {
+    const int mine = kw + 32 * kb + l32;
+    const int j = min(mine, len - 1);
+    live[kb] = mine < len;
+    uint32_t slot = static_cast<uint32_t>(j);
+    if constexpr (kPaged) {
+      const int lb = p.block_shift >= 0 ? j >> p.block_shift : j / p.block_size;
+      const int32_t blk = p.block_table[static_cast<int64_t>(b) * p.max_blocks + lb];
+      const bool ok = blk >= 0 && blk < p.n_blocks;
+      bad_block |= live[kb] && !ok;
+      live[kb] = live[kb] && ok;
+      // (A pool's slots are at least 128 bytes each: below 2^32 of them.)
+      slot = ok ? static_cast<uint32_t>(blk) * static_cast<uint32_t>(p.block_size) +
+                      static_cast<uint32_t>(j - lb * p.block_size) : 0u;
     }
+    const int64_t base = kPaged ? static_cast<int64_t>(p.layer) * p.n_blocks * p.block_size * p.n_kv_heads + kvh
+                                : ((static_cast<int64_t>(b) * p.n_layers + p.layer) * p.n_kv_heads + kvh) * p.s_max;
+    const uint32_t step = kPaged ? static_cast<uint32_t>(p.n_kv_heads) : 1u;
+    char *const to = s_rows + kKeysAt + wave * 32 * kRowBytes;
+#pragma unroll
+    for (int i = 0; i < 32 / kRowsPerLoad; ++i) {
+      const int at = i * kRowsPerLoad + in_load;
+      const uint32_t row = static_cast<uint32_t>(__shfl(static_cast<int>(slot), at));
+      load_to_lds(static_cast<const char *>(p.cache_k) +
+                      (base + static_cast<int64_t>(static_cast<uint64_t>(row) * step)) * kRowBytes +
+                      (chunk ^ (at & (kChunks - 1))) * 16, to + i * 1024);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (a wave reads only what it loaded)
+#pragma unroll
+    for (int i = 0; i < kQ; ++i)
+      k[kb][i] = *reinterpret_cast<const u32x4 *>(to + l32 * kRowBytes + ((kHalf ? 2 * i + half : half * kQ + i) ^ sw) * 16);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (before the next rows, or the tiles, come there)
+  }
+  if (kPaged && p.err != nullptr && __any(bad_block) && lane == 0) atomicOr(p.err, PRCR_DERR_BLOCK);
+  __syncthreads();
+
+  double w[kBlocks] = {};                    // (the first keys add up every row there is: float32 lost 1e-6 of 10,000)
+  if (!kEarly && row0 < n_rows) load_rows(row0, s_rows);
+  int buf = 0, place = 0;                    // of the present tile, among two and three
+  if (threadIdx.x < kRows) {
+    s_lse[0][threadIdx.x] = lse;
+    s_limit[0][threadIdx.x] = limit;
   }
   auto step = [&](int r0, auto is_masked) {
     constexpr bool kMasked = decltype(is_masked)::value;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const bool more = r0 + kRows < n_rows;
+    const int next = place == 2 ? 0 : place + 1;
     if (more) {
-      load_rows(r0 + kRows, s_rows + (buf ^ 1) * kBytes);
+      load_rows(r0 + kRows, s_rows + next * kBytes);
       if (threadIdx.x < kRows) load_lse(r0 + kRows);
     }
 #pragma unroll
     for (int rb = 0; rb < kTileBlocks; ++rb) {
-      const char *const qrow = s_rows + buf * kBytes + (32 * rb + l32) * kRowBytes;
+      const char *const qrow = s_rows + place * kBytes + (32 * rb + l32) * kRowBytes;
       f32x16 s[kBlocks];
 #pragma unroll
       for (int kb = 0; kb < kBlocks; ++kb)
@@ -211,6 +218,7 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
       s_limit[buf ^ 1][threadIdx.x] = limit;
     }
     buf ^= 1;
+    place = next;
   };
   int r0 = row0;
   for (; r0 < n_rows && first + token_of(r0) < k0 + kKeys - 1; r0 += kRows) step(r0, std::true_type{});
@@ -230,15 +238,18 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
 }
 
 // Sum of the workgroups' shares of the rows, a slot per thread.  Slots from the length on
-// have none (the first kernel has written their zeros); a key in a block outside the pool has
-// no weight, whatever was taken for it.
+// have none; a key in a block outside the pool has no weight, whatever was taken for it.
 template <bool kPaged>
 __global__ __launch_bounds__(kThreads) void sum_kernel(const AttendParams p, const Divisor by_blocks, const uint32_t blocks) {
   const uint32_t head = by_blocks.divide(blockIdx.x);
   const int b = static_cast<int>(p.by_heads.divide(head));
   const int j = static_cast<int>(blockIdx.x - head * blocks) * kThreads + static_cast<int>(threadIdx.x);
-  if (j >= clamp_length(p.cache_len[b], p.capacity)) return;
+  if (j >= p.capacity) return;
   const int64_t at = static_cast<int64_t>(head) * p.capacity + j;
+  if (j >= clamp_length(p.cache_len[b], p.capacity)) {
+    if (!p.accumulate) p.weights[at] = 0.f;
+    return;
+  }
   const int64_t step = static_cast<int64_t>(p.batch) * p.n_kv_heads * p.capacity;
   bool live = true;
   if constexpr (kPaged) {
@@ -290,7 +301,7 @@ WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, i
   const int64_t keys = kWaves * 32 * plan.blocks;
   plan.n_stretches = static_cast<int32_t>((capacity + keys - 1) / keys);
   const int64_t have = static_cast<int64_t>(plan.n_stretches) * batch * n_kv_heads;
-  plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>((1024 + have - 1) / have, rows / 512)));
+  plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>((2048 + have - 1) / have, rows / 512)));
   const int64_t elem = dtype == PRCR_F32 ? 4 : 2;
   plan.rotated_bytes = (static_cast<size_t>(total_q) * n_q_heads * head_dim * elem + 255) / 256 * 256;
   plan.bytes = plan.rotated_bytes;
