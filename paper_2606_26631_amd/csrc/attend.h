@@ -71,7 +71,7 @@ struct EvictParams {
 // What a call of chunk attention needs besides its arguments: how its rows and keys are
 // divided, and the bytes of its workspace (partial results of several splits).
 struct ChunkPlan {
-  int32_t waves;                  // per workgroup: a tile is 32 rows a wave
+  bool few;                       // tiles of 32 rows, whose keys the waves share out (or of 128)
   int32_t n_slots, n_split;
   size_t bytes;
 };

@@ -4,9 +4,9 @@
 //   lse = log sum over slots j <= p of exp(s_j),
 // q' the rotated query.  A whole prompt is the case n_b = cache_len[b].
 //
-// A workgroup takes a tile of rows of one sequence and KV head, 32 rows a wave; the rows of a
-// KV head are its tokens' query heads, token by token, so that a tile reads the cache
-// once for all heads of the group.  Tiles of keys and values go through LDS, two of them,
+// A workgroup takes a tile of rows of one sequence and KV head, 32 rows a wave, or, of few
+// rows, 32 for all its waves; the rows of a KV head are its tokens' query heads, token by
+// token, so that a tile reads the cache once for all heads of the group.  Tiles of keys and values go through LDS, two of them,
 // the next one's loads in flight while the present one is used.  The wave forms the scores
 // transposed, K (32 keys) x Q^T (32 rows): a lane then holds scores of one row only (that
 // of its product column), the running maximum and sum of the softmax are one register
@@ -21,6 +21,9 @@
 
 namespace prcr {
 namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
 
 // 16 bytes per lane from memory to LDS: lane l's go to `to` + 16 l.
 __device__ __forceinline__ void load_to_lds(const char *from, char *to) {
@@ -84,17 +87,20 @@ struct TileOf {
   }
 };
 
-template <typename T, int D, bool kPaged, int kWaves>
-__global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_kernel(const AttendParams p) {
+// kFew: one tile of 32 rows for all four waves, which share out its keys' tiles.
+template <typename T, int D, bool kPaged, bool kFew>
+__global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const AttendParams p) {
   using Tile = TileOf<T, D>;
   constexpr bool kHalf = sizeof(T) == 2;     // bf16
-  constexpr int M = 32 * kWaves;
+  constexpr int M = kFew ? 32 : 32 * kWaves;
   constexpr int KT = Tile::kKeys, kRowBytes = Tile::kRowBytes;
   constexpr int KB = KT / 32;                // key blocks of a tile
   constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : (uint64_t{1} << (KT % 64)) - 1;
   constexpr int DT = D / 32;                 // feature blocks
-  constexpr int kMine = Tile::kLoads / kWaves;   // loads of each operand per wave and tile
-  __shared__ __align__(1024) char s_kv[2][2][Tile::kBytes];
+  constexpr int kBy = kFew ? 1 : kWaves;     // waves that load a tile
+  constexpr int kMine = Tile::kLoads / kBy;  // loads of each operand per wave and tile
+  // Two tiles in turn, or (kFew) one of each wave.
+  __shared__ __align__(1024) char s_kv[kFew ? kWaves : 2][2][Tile::kBytes];
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -102,7 +108,7 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   // The lane's rotary pair (one wave read of the arguments, in flight from the start).
   const double freq = p.inv_freq[lane % (D / 2)];
   const int axis = p.axis[lane % (D / 2)];
-  if (blockIdx.x == 0 && p.err != nullptr) report(p, threadIdx.x, kWaves * kWave);
+  if (blockIdx.x == 0 && p.err != nullptr) report(p, threadIdx.x, kThreads);
   const uint32_t id = blockIdx.x;
   const uint32_t by_head = p.by_heads.divide(id);
   const int kvh = static_cast<int>(id - by_head * static_cast<uint32_t>(p.n_kv_heads));
@@ -126,7 +132,7 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   const int t0 = min(split * per, n_tiles), t1 = min(t0 + per, n_tiles);
 
   // The lane's row, and the last slots that it and the wave's last row see.
-  const int wr0 = r0 + wave * 32;
+  const int wr0 = kFew ? r0 : r0 + wave * 32;
   const bool active = wr0 < n_rows;
   const int r = min(wr0 + l32, n_rows - 1);
   const int token = token_of(r);
@@ -139,19 +145,21 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   {
     const char *const at = static_cast<const char *>(p.q) + row * kRowBytes;
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) q[i] = load_nt(at + (2 * i + half) * 16);
+    for (int i = 0; i < kQ; ++i)
+      if (!kFew || i % (kQ / 2) % kWaves == wave) q[i] = load_nt(at + (2 * i + half) * 16);   // (kFew: those it turns)
   }
-  // The wave's tokens, and the positions of the first kTokens of them on the lane's axis (with
-  // 32 pairs, of every second one), in flight before the tile is asked for.
+  // The rows' tokens, eight at a time, a wave's or (kFew) two of them; their positions on the
+  // lane's axis (with 32 pairs, of every second one) are in flight before the tile is asked for.
   constexpr int P = D / 2, kShare = kWave / P;
-  constexpr int kTokens = 2 * Tile::kBytes / kWaves / (P * 16) < 8 ? 2 * Tile::kBytes / kWaves / (P * 16) : 8;
-  static_assert(kTokens >= kShare && (kTokens & (kTokens - 1)) == 0, "tokens of a pass");
+  constexpr int kTokens = 8, kTurns = kTokens / kShare / (kFew ? kWaves : 1);
+  static_assert(kTokens * P * 16 * kWaves <= 2 * Tile::kBytes && kTurns >= 1, "a wave's angles in its share of a tile's buffers");
   const int tok0 = __builtin_amdgcn_readfirstlane(token), tok1 = __builtin_amdgcn_readlane(token, 31);
-  int32_t pos[kTokens / kShare];
+  auto turned = [&](int i) -> int { return ((kFew ? wave * kTurns : 0) + i) * kShare + lane / P; };   // token of eight
+  int32_t pos[kTurns];
   auto load_pos = [&](int c0) {
 #pragma unroll
-    for (int i = 0; i < kTokens / kShare; ++i)
-      pos[i] = p.q_pos[(static_cast<int64_t>(rows.start) + min(c0 + i * kShare + lane / P, tok1)) * 3 + axis];
+    for (int i = 0; i < kTurns; ++i)
+      pos[i] = p.q_pos[(static_cast<int64_t>(rows.start) + min(c0 + turned(i), tok1)) * 3 + axis];
   };
   load_pos(tok0);
 
@@ -188,7 +196,7 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
     }
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-      const int load = i * kWaves + wave;
+      const int load = kFew ? i : i * kWaves + wave;
       const int at = load * Tile::kRowsPerLoad + in_load;        // the lane's row of the tile
       int64_t from;
       if constexpr (kPaged)
@@ -209,31 +217,45 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = -FLT_MAX, l = 0.f;               // running maximum (base 2), the lane's own keys' sum
 
+  // The wave's first tile, and the tiles from one of its own to the next.
+  const int tw = kFew ? t0 + wave : t0;
+  constexpr int kStep = kFew ? kWaves : 1;
   uint64_t live = ~uint64_t{0}, live_next = ~uint64_t{0};
-  if (t0 < t1) {
-    if constexpr (kPaged) entry = entry_of(t0, &entry_off);
-    live_next = load_tile(t0, s_kv[t0 & 1]);
-    if constexpr (kPaged) entry = entry_of(min(t0 + 1, t1 - 1), &entry_off);
+  if (tw < t1) {
+    if constexpr (kPaged) entry = entry_of(tw, &entry_off);
+    live_next = load_tile(tw, s_kv[kFew ? wave : tw & 1]);
+    if constexpr (kPaged) entry = entry_of(min(tw + kStep, t1 - 1), &entry_off);
   }
 
   // The rows are turned while the first tile comes: in double precision, rounded once to the
   // stored type, as prefill capture rotates the keys.  (The matrix products take operands
   // of that type, so a query is rounded to it at some point; rounded here, the scores are those
-  // of two rows of the same kind, and their sums stay in float32.)  The wave's tokens' cosines
-  // and sines go through its share of the second tile's buffer, a few tokens at a time, since
-  // the rows of a group share them; a pair's place is permuted by the token, for the banks.
+  // of two rows of the same kind, and their sums stay in float32.)  The tokens' cosines and
+  // sines go through LDS (the second tile's buffer, a share of it for each wave), since the
+  // rows of a group share them; a pair's place is permuted by the token, for the banks.  kFew:
+  // the waves share that work too, and the turned rows pass through LDS to all of them.
   if (active && t0 < t1) {
     constexpr int kPer = Store<T>::kPerChunk;
     // A pair's cosine and sine, 16 bytes: doubles, or (bf16) as two floats each.
     typedef double f64x2 __attribute__((ext_vector_type(2)));
-    f64x2 *const table = reinterpret_cast<f64x2 *>(&s_kv[(t0 + 1) & 1][0][0] + wave * (2 * Tile::kBytes / kWaves));
+    __shared__ __align__(16) f64x2 s_angles[kFew ? kTokens * P : 1];
+    __shared__ __align__(16) char s_turned[kFew ? 32 : 1][kRowBytes];
+    f64x2 *const table = kFew ? s_angles
+                              : reinterpret_cast<f64x2 *>(&s_kv[(t0 + 1) & 1][0][0] + wave * (2 * Tile::kBytes / kWaves));
+    // The angles' writes before their reads, and those before the next ones' writes.
+    auto sync = [&] {
+      if constexpr (kFew)
+        __syncthreads();
+      else
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the wave's own)
+    };
     for (int c0 = tok0; c0 <= tok1; c0 += kTokens) {
       const int n = min(kTokens, tok1 + 1 - c0);
       if (c0 != tok0) load_pos(c0);
 #pragma unroll
-      for (int i = 0; i < kTokens / kShare; ++i) {
-        const int tok = i * kShare + lane / P;
-        if (i * kShare >= n) break;          // (past the wave's last token: not read)
+      for (int i = 0; i < kTurns; ++i) {
+        const int tok = turned(i);
+        if ((tok & -kShare) >= n) break;     // (past the last token: not read)
         double sn, cs;
         turn(static_cast<double>(pos[i]) * freq, &sn, &cs);
         if (p.negate) {
@@ -244,11 +266,12 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
         if constexpr (kHalf) both = __builtin_bit_cast(f64x2, split_angle(cs, sn));
         table[tok * P + (lane % P ^ (tok & 7))] = both;
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own writes)
+      sync();
       const int tok = token - c0;
       if (tok >= 0 && tok < n) {
 #pragma unroll
         for (int i = 0; i < kQ / 2; ++i) {
+          if (kFew && i % kWaves != wave) continue;
           f64x2 angle[kPer];
 #pragma unroll
           for (int e = 0; e < kPer; ++e) angle[e] = table[tok * P + (((2 * i + half) * kPer + e) ^ (tok & 7))];
@@ -271,25 +294,35 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
           }
         }
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (its reads, before the next tokens)
+      sync();
+    }
+    if constexpr (kFew) {
+      const int sw = Tile::key_swizzle(l32);
+#pragma unroll
+      for (int i = 0; i < kQ; ++i)
+        if (i % (kQ / 2) % kWaves == wave) *reinterpret_cast<u32x4 *>(&s_turned[l32][((2 * i + half) ^ sw) * 16]) = q[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kQ; ++i) q[i] = *reinterpret_cast<const u32x4 *>(&s_turned[l32][((2 * i + half) ^ sw) * 16]);
     }
   }
   // One tile.  The first tiles, which every row sees whole, have neither the mask nor, between
   // their reads and products, what is done for it: kMasked is right for every tile.
   auto step = [&](int t, auto is_masked) {
     constexpr bool kMasked = decltype(is_masked)::value;
-    // The tile's loads have arrived, in every wave, and every wave is done with the other buffer.
+    // The tile's loads have arrived, in every wave (kFew: the wave's own), and every wave is done
+    // with the other buffer.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    if constexpr (!kFew) __syncthreads();
     live = live_next;
-    if (t + 1 < t1) {
+    if (!kFew && t + 1 < t1) {
       live_next = load_tile(t + 1, s_kv[(t + 1) & 1]);
       if constexpr (kPaged) entry = entry_of(min(t + 2, t1 - 1), &entry_off);
     }
     const int k0 = t * KT;
     if (!active || (kMasked && k0 > wmax)) return;
-    const char *const kt = s_kv[t & 1][0];
-    const char *const vt = s_kv[t & 1][1];
+    const char *const kt = s_kv[kFew ? wave : t & 1][0];
+    const char *const vt = s_kv[kFew ? wave : t & 1][1];
 
     // Scores: lane's keys 32 kb + 8 (i / 4) + 4 half + i % 4 of row l32.
     f32x16 s[KB];
@@ -456,15 +489,84 @@ __global__ __launch_bounds__(kWaves * kWave, kWaves == 1 ? 1 : 2) void chunk_ker
   };
   // Tiles that the workgroup's first row sees whole.
   const int t_whole = min(t1, max(t0, (first + token_of(r0) + 1) / KT));
-  int t = t0;
-  for (; t < t_whole; ++t) {
-    if (kPaged && (live_next & kAll) != kAll) break;                                // (a block outside the pool; the same in every wave)
+  // (kFew: the wave's next tile, once this one's buffer has been read.)
+  auto next_tile = [&](int t) {
+    if (!kFew || t + kStep >= t1) return;
+    live_next = load_tile(t + kStep, s_kv[wave]);
+    if constexpr (kPaged) entry = entry_of(min(t + 2 * kStep, t1 - 1), &entry_off);
+  };
+  int t = tw;
+  for (; t < t_whole; t += kStep) {
+    if (kPaged && (live_next & kAll) != kAll) break;         // (a block outside the pool; the same in every wave of a tile)
     step(t, std::false_type{});
+    next_tile(t);
   }
-  for (; t < t1; ++t) step(t, std::true_type{});
+  for (; t < t1; t += kStep) {
+    step(t, std::true_type{});
+    next_tile(t);
+  }
   if (kPaged && p.err != nullptr && __any(bad_block) && lane == 0) atomicOr(p.err, PRCR_DERR_BLOCK);
 
   l = half_sum(l);
+  if constexpr (kFew) {
+    // The waves' sums, through the tiles' buffers; a thread then has 1 / 8 of a row's features.
+    constexpr int kRow = D + 4, F = D / 8;   // floats (padded for the banks)
+    __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+    static_assert(32 * kRow * 4 <= 2 * Tile::kBytes, "a wave's sums in its tile's buffers");
+    float *const mine = reinterpret_cast<float *>(&s_kv[wave][0][0]);
+    if (half == 0) {
+      s_m[wave][l32] = m;
+      s_l[wave][l32] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4 *>(mine + l32 * kRow + 32 * d + 8 * i + 4 * half) =
+            f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    __syncthreads();
+    const int at = threadIdx.x / 8, from = static_cast<int>(threadIdx.x) % 8 * F;
+    if (r0 + at >= n_rows) return;
+    float ms = -FLT_MAX, ls = 0.f, x[F] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) ms = s_l[w][at] != 0.f ? fmaxf(ms, s_m[w][at]) : ms;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float lw = s_l[w][at];
+      if (lw == 0.f) continue;               // (no key: no features either)
+      const float f = exp2_hw(s_m[w][at] - ms);
+      ls = fmaf(lw, f, ls);
+      const float *const o_w = reinterpret_cast<const float *>(&s_kv[w][0][0]) + at * kRow + from;
+#pragma unroll
+      for (int e = 0; e < F; ++e) x[e] = fmaf(o_w[e], f, x[e]);
+    }
+    const int tok = token_of(r0 + at);
+    const int64_t of = (static_cast<int64_t>(rows.start) + tok) * p.n_q_heads + kvh * G + (r0 + at - tok * G);
+    if (p.n_split > 1) {
+      float *const part = p.part + (of * p.n_split + split) * (D + 2);
+      if (from == 0) {
+        part[D] = ms;
+        part[D + 1] = ls;
+      }
+#pragma unroll
+      for (int e = 0; e < F; e += 2) *reinterpret_cast<f32x2 *>(part + from + e) = f32x2{x[e], x[e + 1]};
+      return;
+    }
+    if (p.lse != nullptr && from == 0)
+      p.lse[of] = ls != 0.f ? (ms + __builtin_amdgcn_logf(ls)) * 0.693147180559945309f : -__builtin_inff();
+    char *const out = static_cast<char *>(p.out) + of * kRowBytes + from * static_cast<int>(sizeof(T));
+#pragma unroll
+    for (int e = 0; e < F; ++e) x[e] = ls != 0.f ? x[e] / ls : 0.f;
+    if constexpr (kHalf) {
+#pragma unroll
+      for (int e = 0; e < F; e += 4)
+        *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{pack_bf16(x[e], x[e + 1]), pack_bf16(x[e + 2], x[e + 3])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < F; e += 4) *reinterpret_cast<f32x4 *>(out + 4 * e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+    }
+    return;
+  }
   if (!active || wr0 + l32 >= n_rows) return;
   if (p.n_split > 1) {
     float *const part = p.part + (row * p.n_split + split) * (D + 2);
@@ -577,12 +679,12 @@ hipError_t chunk(const AttendParams &p, const ChunkPlan &plan, hipStream_t strea
   const int64_t blocks = static_cast<int64_t>(p.n_kv_heads) * p.n_slots * p.n_split;
   const int64_t rows = static_cast<int64_t>(p.total_q) * p.n_q_heads;
   const int64_t merges = (rows + kMergeWaves - 1) / kMergeWaves;
-  if (blocks > INT32_MAX || !grid_fits(blocks, plan.waves * kWave) || (p.n_split > 1 && !grid_fits(merges, kMergeWaves * kWave)))
+  if (blocks > INT32_MAX || !grid_fits(blocks, kThreads) || (p.n_split > 1 && !grid_fits(merges, kMergeWaves * kWave)))
     return hipErrorInvalidConfiguration;
-  if (plan.waves == 1)
-    chunk_kernel<T, D, kPaged, 1><<<static_cast<unsigned>(blocks), kWave, 0, stream>>>(p);
+  if (plan.few)
+    chunk_kernel<T, D, kPaged, true><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p);
   else
-    chunk_kernel<T, D, kPaged, 4><<<static_cast<unsigned>(blocks), 4 * kWave, 0, stream>>>(p);
+    chunk_kernel<T, D, kPaged, false><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
   merge_kernel<T, D><<<static_cast<unsigned>(merges), kMergeWaves * kWave, 0, stream>>>(p);
@@ -601,16 +703,22 @@ ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n
   ChunkPlan plan{};
   const int64_t group = n_q_heads / n_kv_heads;
   const int64_t rows = static_cast<int64_t>(total_q) * group;
-  plan.waves = rows <= int64_t{64} * batch ? 1 : 4;
-  plan.n_slots = static_cast<int32_t>(rows / (32 * plan.waves)) + batch;
+  // Tiles of 32 rows whose keys the waves share out, where a sequence has two of them at most
+  // or where all tiles of 128 rows together would not be a workgroup on every second
+  // compute unit.
+  plan.few = rows <= int64_t{64} * batch || (rows / (32 * kWaves) + batch) * n_kv_heads < 128;
+  plan.n_slots = static_cast<int32_t>(rows / (plan.few ? 32 : 32 * kWaves)) + batch;
   // A call of too few tiles for two workgroups per compute unit splits the keys, by what that
-  // costs: a workgroup takes about a microsecond for 64 keys, and every split writes and reads
-  // a partial result of 4 (D + 2) bytes per row and head, at some 4 MB a microsecond.  (The
-  // lengths are on the device: the capacity stands for them.)
+  // costs: a workgroup takes about a microsecond for 64 keys (of each wave, where they
+  // share them out), and every split writes and reads a partial result of 4 (D + 2) bytes per row
+  // and head, at some 16 MB a microsecond.  The merge is a launch more, about four
+  // microseconds: two rounds or fewer are not split.  (The lengths are on the device: the
+  // capacity stands for them.)
   const int64_t have = static_cast<int64_t>(plan.n_slots) * n_kv_heads;
-  const double tiles = static_cast<double>(capacity) / 64, rows_all = static_cast<double>(total_q) * n_q_heads;
-  const double best = std::sqrt(tiles * 4e6 / (rows_all * 8 * (head_dim + 2)));
-  const int64_t most = std::min<int64_t>({(512 + have - 1) / have, (capacity + 63) / 64, kMostSplits});
+  const int64_t keys = plan.few ? 64 * kWaves : 64;          // of a workgroup at a time
+  const double rounds = static_cast<double>(capacity) / keys, rows_all = static_cast<double>(total_q) * n_q_heads;
+  const double best = rounds <= 2 ? 1 : std::sqrt(rounds * 16e6 / (rows_all * 8 * (head_dim + 2)));
+  const int64_t most = std::min<int64_t>({(512 + have - 1) / have, (capacity + keys - 1) / keys, kMostSplits});
   plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most, static_cast<int64_t>(best))));
   if (plan.n_split > 1) plan.bytes = static_cast<size_t>(total_q) * n_q_heads * plan.n_split * (head_dim + 2) * 4;
   return plan;
