@@ -6,8 +6,10 @@
 //
 // A workgroup takes a tile of rows of one sequence and KV head, 32 rows a wave, or, of few
 // rows, 32 for all its waves; the rows of a KV head are its tokens' query heads, token by
-// token, so that a tile reads the cache once for all heads of the group.  Tiles of keys and values go through LDS, two of them,
-// the next one's loads in flight while the present one is used.  The wave forms the scores
+// token, so that a tile reads the cache once for all heads of the group.  Tiles of keys and
+// values go through LDS, two of them, the next one's loads in flight while the present one is
+// used: a tile of 64 keys is used by 128 rows, so that LDS is filled at a sixth of what it
+// is read at, and two workgroups with their 128 registers a lane fit a compute unit.  The wave forms the scores
 // transposed, K (32 keys) x Q^T (32 rows): a lane then holds scores of one row only (that
 // of its product column), the running maximum and sum of the softmax are one register
 // each, and the weights are, in the registers where they arise, the operand of the value
@@ -31,12 +33,15 @@ __device__ __forceinline__ void load_to_lds(const char *from, char *to) {
                                    (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
 
-// The sequence that tile slot `slot` belongs to, and what the tile has to know of it.
-// Sequence b has the slots from floor(q_off[b] G / M) + b on, enough of them for its rows'
-// tiles of M.  Up to 64 sequences are one round of loads, a sequence per lane: every round costs
-// about a microsecond before the first key.
+// The sequence of the workgroup that comes `order`-th, and what the tile has to know of it.  The
+// last tiles, which of a prompt see the most keys, come first.  Up to 64 sequences are one round of loads,
+// a sequence per lane (every round costs about a microsecond before the first key), and
+// their tiles are counted: tile slots are one behind the other, the workgroups without one at the end.
+// Between the others, such workgroups left dies idle: 64 sequences of 32 rows, every second slot
+// empty, took 137 us (float32, 1,160 slots) and now take 80.  Of more sequences, sequence b has the slots from
+// floor(q_off[b] G / M) + b on, enough of them for its rows' tiles of M.
 struct Sequence {
-  int b, slot0;                              // and its first slot
+  int b, tile;                               // and the workgroup's tile of its rows (none: below 0)
   Rows rows;
   int32_t len;
 };
@@ -44,10 +49,22 @@ template <int M>
 __device__ __forceinline__ int32_t first_slot(const AttendParams &p, int b, int32_t off) {
   return static_cast<int32_t>(static_cast<uint32_t>(min(max(off, 0), p.total_q)) * static_cast<uint32_t>(p.group) / M) + b;
 }
+// Sum over the lanes up to each: within rows of 16, then the rows' last lanes onto the next ones.
+__device__ __forceinline__ int running_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // from 1, 2, 4, 8 lanes below
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row 0's sum to row 1, 2's to 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // the lower half's to the upper one
+  return x;
+}
 template <int M>
-__device__ __forceinline__ Sequence sequence_of_slot(const AttendParams &p, int lane, int slot) {
-  int lo = 0, n = p.batch;                   // among sequences lo .. lo + n - 1, the last that starts by `slot`
-  while (n > kWave) {
+__device__ __forceinline__ Sequence sequence_of(const AttendParams &p, int lane, int order) {
+  int lo = 0, n = p.batch;                   // among sequences lo .. lo + n - 1
+  int slot = p.n_slots - 1 - order;
+  const bool counted = n <= kWave;
+  while (n > kWave) {                        // the last that starts by `slot`
     const int step = (n + kWave - 1) / kWave;
     const int b = lo + lane * step;
     const bool ok = lane * step < n && first_slot<M>(p, b, p.q_off[b]) <= slot;
@@ -58,11 +75,21 @@ __device__ __forceinline__ Sequence sequence_of_slot(const AttendParams &p, int 
   const int b = lo + min(lane, n - 1);
   const Rows rows = rows_of(p, b);
   const int32_t len = clamp_length(p.cache_len[b], p.capacity);
-  const int32_t slot0 = first_slot<M>(p, b, rows.start);
-  const int k = max(__popcll(__ballot(lane < n && slot0 <= slot)) - 1, 0);
+  int tile, k;
+  if (counted) {
+    const int tiles = lane < n ? (rows.n * p.group + M - 1) / M : 0;
+    const int end = running_sum(tiles);
+    slot = __builtin_amdgcn_readlane(end, kWave - 1) - 1 - order;
+    tile = slot - (end - tiles);
+    const uint64_t mine = __ballot(tile >= 0 && tile < tiles);
+    k = mine != 0 ? __ffsll(static_cast<unsigned long long>(mine)) - 1 : 0;
+  } else {
+    tile = slot - first_slot<M>(p, b, rows.start);
+    k = max(__popcll(__ballot(lane < n && tile >= 0)) - 1, 0);
+  }
   Sequence s;
   s.b = __builtin_amdgcn_readfirstlane(lo + k);
-  s.slot0 = __builtin_amdgcn_readlane(slot0, k);
+  s.tile = __builtin_amdgcn_readlane(tile, k);
   s.rows = Rows{__builtin_amdgcn_readlane(rows.start, k), __builtin_amdgcn_readlane(rows.n, k), false};
   s.len = __builtin_amdgcn_readlane(len, k);
   return s;
@@ -114,15 +141,15 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
   const int kvh = static_cast<int>(id - by_head * static_cast<uint32_t>(p.n_kv_heads));
   const uint32_t by_split = p.by_split.divide(by_head);
   const int split = static_cast<int>(by_head - by_split * static_cast<uint32_t>(p.n_split));
-  const int slot = p.n_slots - 1 - static_cast<int>(by_split);   // a prompt's last tiles see the most keys: first
-  const Sequence seq = sequence_of_slot<M>(p, lane, slot);
+  const Sequence seq = sequence_of<M>(p, lane, static_cast<int>(by_split));
   const int b = seq.b;
   const Rows rows = seq.rows;
   const int32_t len = seq.len;
   const int G = p.group;
   const int n_rows = rows.n * G;
-  const int r0 = (slot - seq.slot0) * M;
-  if (r0 < 0 || r0 >= n_rows) return;
+  if (seq.tile < 0) return;
+  const int r0 = seq.tile * M;
+  if (r0 >= n_rows) return;
 
   const int first = len - rows.n;            // slot of the sequence's first row
   auto token_of = [&](int r) -> int { return static_cast<int>(p.by_group.divide(static_cast<uint32_t>(r))); };
@@ -703,22 +730,29 @@ ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n
   ChunkPlan plan{};
   const int64_t group = n_q_heads / n_kv_heads;
   const int64_t rows = static_cast<int64_t>(total_q) * group;
-  // Tiles of 32 rows whose keys the waves share out, where a sequence has two of them at most
-  // or where all tiles of 128 rows together would not be a workgroup on every second
-  // compute unit.
-  plan.few = rows <= int64_t{64} * batch || (rows / (32 * kWaves) + batch) * n_kv_heads < 128;
-  plan.n_slots = static_cast<int32_t>(rows / (plan.few ? 32 : 32 * kWaves)) + batch;
-  // A call of too few tiles for two workgroups per compute unit splits the keys, by what that
-  // costs: a workgroup takes about a microsecond for 64 keys (of each wave, where they
-  // share them out), and every split writes and reads a partial result of 4 (D + 2) bytes per row
-  // and head, at some 16 MB a microsecond.  The merge is a launch more, about four
-  // microseconds: two rounds or fewer are not split.  (The lengths are on the device: the
-  // capacity stands for them.)
-  const int64_t have = static_cast<int64_t>(plan.n_slots) * n_kv_heads;
+  // Workgroups for all rows and heads in tiles of m rows, of sequences of the same length.
+  auto tiles = [&](int64_t m) { return std::max<int64_t>(batch * ((rows + m * batch - 1) / (m * batch)) * n_kv_heads, 1); };
+  // Tiles of 32 rows whose keys the waves share out take a compute unit each (their LDS): where
+  // one round of them does it.  bf16, 8 KV heads of 4 query heads, 4,000 cached slots, both ways:
+  // one sequence of 40 rows, 40 workgroups, 18 and 30 us; 16 sequences of 16, 256 workgroups, 50
+  // and 56; 4 sequences of 120, 480 workgroups, 82 and 66.
+  plan.few = tiles(32) <= 256;
+  const int64_t tile = plan.few ? 32 : 32 * kWaves, have = tiles(tile);
+  plan.n_slots = static_cast<int32_t>(rows / tile) + batch;
+  // The keys are split for as many workgroups as run at a time (few rows: one per
+  // compute unit, else two), or, of fewer, by what that costs: a workgroup takes about a
+  // microsecond for 64 keys (of each wave, where they share them out), and every split
+  // writes and reads a partial result of 4 (D + 2) bytes per row and head, at some 16 MB a
+  // microsecond, or 4 MB where a workgroup writes those of 128 rows at its end (one sequence
+  // of 40 rows over 1,192 slots: 13.4 us with 16, 14.9 with 4; of 400 rows over 500 slots: 21 us
+  // with 4, 27 with 16; over 1,552 slots 35 with 4, 36 with 16, 41 with 1).  The merge is
+  // a launch more, about four microseconds: two rounds or fewer are not split.  A round that is
+  // not full is better than two: one sequence of 400 rows over 4,400 slots, 104 workgroups, takes
+  // 61 us in 4 splits, 70 in 5.  (The lengths are on the device: the capacity stands for them.)
   const int64_t keys = plan.few ? 64 * kWaves : 64;          // of a workgroup at a time
   const double rounds = static_cast<double>(capacity) / keys, rows_all = static_cast<double>(total_q) * n_q_heads;
-  const double best = rounds <= 2 ? 1 : std::sqrt(rounds * 16e6 / (rows_all * 8 * (head_dim + 2)));
-  const int64_t most = std::min<int64_t>({(512 + have - 1) / have, (capacity + keys - 1) / keys, kMostSplits});
+  const double best = rounds <= 2 ? 1 : std::sqrt(rounds * (plan.few ? 16e6 : 4e6) / (rows_all * 8 * (head_dim + 2)));
+  const int64_t most = std::min<int64_t>({(plan.few ? 256 : 512) / have, (capacity + keys - 1) / keys, kMostSplits});
   plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most, static_cast<int64_t>(best))));
   if (plan.n_split > 1) plan.bytes = static_cast<size_t>(total_q) * n_q_heads * plan.n_split * (head_dim + 2) * 4;
   return plan;

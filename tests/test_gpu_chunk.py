@@ -134,6 +134,29 @@ def test_many_sequences(B):
     check(out, lse, x.expect())
 
 
+@pytest.mark.parametrize("block", [0, 16])
+def test_rows_that_fill_their_tiles(block):
+    """64 sequences of which some have exactly one tile of 32 or 128 rows, or a row more, or none."""
+    print(f"whole tiles, block {block}", flush=True)
+    ns = np.array([32, 0, 33, 1, 31, 128, 0, 129, 64, 16] * 6 + [0, 0, 32, 5])
+    x = Inputs("bf16", 64, 2, 1, ns, ns + np.arange(64) % 7 * 40, block, seed=21)
+    out, lse, err = run(x)
+    assert err == 0
+    check(out, lse, x.expect())
+
+
+@pytest.mark.parametrize("H,G,n,past", [(4, 7, 400, 1500), (8, 4, 400, 100), (2, 4, 40, 4000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_and_keys_shared_out(dtype, H, G, n, past):
+    """One sequence: tiles of 128 rows, or of 32, with the keys split."""
+    print(f"shared out {dtype} {H} {G} {n} {past}", flush=True)
+    x = Inputs(dtype, 64, H, G, [n], [n + past], seed=n + past, layers=1)
+    assert prcr.chunk_workspace_bytes(x.cache(), x.q.shape[0], H * G) > 0
+    out, lse, err = run(x)
+    assert err == 0
+    check(out, lse, x.expect())
+
+
 def test_padded_rows():
     """A padded [B, S] batch: offsets b S and the rows' counts; padding is left as it is."""
     S, n = 9, np.array([9, 4, 0, 1], np.int32)
