@@ -382,7 +382,8 @@ prcr_status prcr_decode_attention_static(const prcr_rope *rope, const prcr_cache
  * (s_max, or max_blocks * block_size) and total_q * n_q_heads are at most 2^30, else
  * PRCR_ERR_SHAPE; head_dim 64 or 128 and the axis maps of prcr_rebind_inject.  A cache_len beyond
  * the capacity is clamped with PRCR_DERR_CAPACITY; a sequence with malformed offsets or
- * q_len has no rows (PRCR_DERR_OFFSETS); a block-table entry outside the pool skips its keys
+ * q_len has no rows (PRCR_DERR_OFFSETS; where q_off decreases, the outputs of the other rows
+ * are unspecified); a block-table entry outside the pool skips its keys
  * (PRCR_DERR_BLOCK).  Outputs and workspace must not share memory with an input or
  * with each other (PRCR_ERR_ALIAS).  total_q = 0 is allowed.
  */
@@ -429,7 +430,7 @@ prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, int32_t batch,
  *                 were.  accumulate == 0: every slot is written, 0 from cache_len[b] on.
  *   workspace     prcr_key_weights_workspace_size() bytes, 16-byte aligned
  * Rows are summed 16 at a time in float32 and those sums in double, in an order that depends
- * on the lengths alone; the result is rounded to float32 and added.  A row with lse =
+ * on shapes and lengths alone; the result is rounded to float32 and added.  A row with lse =
  * -infinity sees nothing and gives nothing.
  */
 prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache,
@@ -460,7 +461,7 @@ prcr_status prcr_key_weights_workspace_size(const prcr_cache *cache, prcr_dtype 
  * key was rotated at the token's own position, which stays).
  *
  *   weights        float32 [batch][n_kv_heads][capacity], as prcr_key_weights fills them
- *   budget         >= 1;  keep_first, keep_last >= 0, their sum at most budget
+ *   budget         1 to 2^30;  keep_first, keep_last >= 0, their sum at most budget
  *   new_cache_len  out int32 [batch]: min(cache_len[b], budget); may be cache_len itself
  *   kept           out int32 [batch][budget]: the kept slots, ascending, then -1
  *   new_weights    out, as weights, or NULL: the kept slots' weights at their new slots, 0 from
@@ -472,8 +473,8 @@ prcr_status prcr_key_weights_workspace_size(const prcr_cache *cache, prcr_dtype 
  *                  be given: their slots are wrong after the call otherwise.
  *   workspace      prcr_evict_workspace_size() bytes, 8-byte aligned
  * Rows of slots from new_cache_len[b] on are left as they are.  Paged: the block table stays; blocks
- * past the new length are the caller's to reuse, and a sequence's blocks must not be
- * another one's too.  A block-table entry outside the pool skips its rows (PRCR_DERR_BLOCK).
+ * past the new length are the caller's to reuse, and a block must not be
+ * another sequence's too, nor twice in one.  A block-table entry outside the pool skips its rows (PRCR_DERR_BLOCK).
  * No output may share memory with another array (PRCR_ERR_ALIAS), but new_cache_len be cache_len.
  */
 prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,

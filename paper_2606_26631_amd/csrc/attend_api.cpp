@@ -11,7 +11,7 @@ using namespace prcr;
 
 namespace {
 
-constexpr int64_t kMaxSlots = int64_t{1} << 30;    // cache capacity per sequence, and rows per KV head
+constexpr int64_t kMaxSlots = int64_t{1} << 30;    // cache capacity per sequence, rows per KV head, and budget
 
 bool aligned(const void *p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -93,7 +93,8 @@ prcr_status prepare(const prcr_rope *rope, const prcr_cache *cache, prcr_dtype d
   if ((st = check_cache(cache, &capacity)) != PRCR_OK) return st;
   if (q_off == nullptr || cache_len == nullptr) return PRCR_ERR_NULL;
   if (total_q > 0 && (q == nullptr || q_pos == nullptr)) return PRCR_ERR_NULL;
-  if (n_layers < 1 || layer < 0 || layer >= n_layers || !std::isfinite(scale)) return PRCR_ERR_SHAPE;
+  if (n_layers < 1 || layer < 0 || layer >= n_layers) return PRCR_ERR_SHAPE;
+  if (!std::isfinite(scale) || !std::isfinite(scale * 1.4426950408889634f)) return PRCR_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(q_off, 4) || !aligned(q_len, 4) || !aligned(q_pos, 4) || !aligned(cache_len, 4) ||
       !aligned(workspace, 16) || !aligned(err_flag, 4))
     return PRCR_ERR_ALIGN;
@@ -251,7 +252,7 @@ prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch, in
   int64_t capacity = 0;
   prcr_status st = check_heads(batch, 1, 64);
   if (st == PRCR_OK) st = cache_shape(cache, &capacity);
-  if (st == PRCR_OK && budget < 1) st = PRCR_ERR_SHAPE;
+  if (st == PRCR_OK && (budget < 1 || budget > kMaxSlots)) st = PRCR_ERR_SHAPE;
   if (st != PRCR_OK) return st;
   // Paged: a kept slot's two places; then the scores; then the first slots that move.
   *bytes = static_cast<size_t>(batch) * ((cache->paged ? static_cast<size_t>(budget) * 8 : 0) +
@@ -281,7 +282,7 @@ prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
   const bool rename = mem != nullptr && mem->v == nullptr;
   if (rename) {
     if (mem->v_slot == nullptr) return PRCR_ERR_NULL;
-    if (mem->batch != batch || mem->max_visual < 1) return PRCR_ERR_SHAPE;
+    if (mem->batch != batch || mem->max_visual < 1 || mem->max_visual > kMaxSlots) return PRCR_ERR_SHAPE;
     if (!aligned(mem->v_slot, 4)) return PRCR_ERR_ALIGN;
   }
   if (!aligned(cache_len, 4) || !aligned(weights, 4) || !aligned(new_cache_len, 4) || !aligned(kept, 4) ||

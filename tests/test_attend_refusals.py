@@ -73,9 +73,9 @@ def test_both(fn, case):
     (dict(out=None), NULL), (dict(ws=None), NULL), (dict(bytes=0), SHAPE), (dict(out=AT["out"] + 8), ALIGN),
     (dict(out=AT["q"]), ALIAS), (dict(out=AT["k"] + 16), ALIAS), (dict(lse=AT["out"] + 256), ALIAS),
     (dict(ws=AT["v"]), ALIAS), (dict(lse=AT["q_off"] + 8), ALIAS), (dict(out=AT["cache_len"] - 16), ALIAS),
-    (dict(cache=paged(), ws=AT["table"] + 128), ALIAS), (dict(out=AT["q_pos"]), ALIAS), (dict(lse=AT["q_len"]), ALIAS)])
+    (dict(cache=paged(max_blocks=256), ws=AT["table"] + 128), ALIAS), (dict(out=AT["q_pos"]), ALIAS), (dict(lse=AT["q_len"]), ALIAS)])
 def test_chunk(kw, want):
-    kw = dict(total_q=10, cache=contiguous()) | kw       # (few rows: the keys are split)
+    kw = dict(total_q=10, cache=contiguous(4096)) | kw   # (few rows, many slots: the keys are split)
     assert attend("chunk", **kw) == want
 
 
@@ -122,6 +122,22 @@ def memory(batch=2, max_visual=9, v=None, v_slot=AT["v_slot"]):
     (dict(cache=paged(), kept=AT["table"]), ALIAS), (dict(mem=memory(v_slot=AT["cache_len"])), ALIAS)])
 def test_evict(kw, want):
     assert evict(**kw) == want
+
+
+@pytest.mark.parametrize("kw", [dict(budget=(1 << 30) + 1), dict(budget=2 ** 31 - 1),
+                                dict(mem=memory(max_visual=(1 << 30) + 1)), dict(mem=memory(max_visual=2 ** 31 - 1))])
+def test_evict_counts_beyond_the_largest(kw):
+    """Counts that a loop's 32-bit index could run past."""
+    assert evict(bytes=1 << 40, **kw) == SHAPE
+    n = ctypes.c_size_t()
+    if "budget" in kw:
+        assert prcr.lib().prcr_evict_workspace_size(ctypes.byref(contiguous()), 2, kw["budget"], ctypes.byref(n)) == SHAPE
+
+
+@pytest.mark.parametrize("fn", ["chunk", "weights"])
+@pytest.mark.parametrize("scale", [3e38, -3e38])
+def test_scale_without_a_finite_base_two_form(fn, scale):
+    assert attend(fn, scale=scale) == SHAPE
 
 
 def test_workspace_sizes():
