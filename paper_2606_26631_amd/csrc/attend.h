@@ -78,8 +78,8 @@ struct ChunkPlan {
 ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
                      int32_t head_dim);
 
-// The same of the keys' weights (rotated queries, then partial sums): 32-key blocks a wave holds, key stretches of a sequence, and
-// the workgroups that share a stretch's rows.
+// The same of the keys' weights (rotated queries, then partial sums): 32-key blocks a wave
+// holds, key stretches of a sequence, and the workgroups that share a stretch's rows.
 struct WeightsPlan {
   int32_t blocks, n_stretches, n_split;
   size_t rotated_bytes, bytes;

@@ -10,6 +10,10 @@
 // their weights in its own registers: no other lane's, no atomics, a fixed order.  Where
 // that makes few workgroups, the rows are shared out over several, whose sums a second
 // kernel adds in order.
+//
+// What bounds it: of few rows, reading the keys (one token of 32 sequences of 3,500 slots, 8 heads of
+// 128: 230 MB in 50 us, 4.6 TB/s); of many, an exponential and a sum per score beside the products
+// (4 prompts of 2,560 tokens, 32 heads: 147 us, 0.73 PF of products).
 #include <algorithm>
 #include <type_traits>
 
@@ -297,11 +301,22 @@ WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, i
   int64_t tokens = (static_cast<int64_t>(total_q) + batch - 1) / batch;
   if (window > 0) tokens = std::min<int64_t>(tokens, window);
   const int64_t rows = tokens * (n_q_heads / n_kv_heads);     // of a sequence and KV head, on average
-  plan.blocks = dtype == PRCR_BF16 && rows > 512 ? 2 : 1;
-  const int64_t keys = kWaves * 32 * plan.blocks;
-  plan.n_stretches = static_cast<int32_t>((capacity + keys - 1) / keys);
-  const int64_t have = static_cast<int64_t>(plan.n_stretches) * batch * n_kv_heads;
-  plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>((2048 + have - 1) / have, rows / 512)));
+  // Two key blocks a wave use a row tile's read for both, but make half as many workgroups: for
+  // long runs, counted as rows times stretches of 128 keys.  bf16, 8 KV heads of 4 query heads:
+  // 4 prompts of 2,560 tokens (6.6 million) take 203 us with two and 211 with one; one
+  // prompt of 1,000 (0.3 million) 39 and 34; 250 tokens over 1,400 slots of 16 sequences
+  // (1.4 million) 95 and 96.  (float32, whose keys would take 256 registers, has one.)
+  auto stretches = [&](int64_t blocks) { return (capacity + kWaves * 32 * blocks - 1) / (kWaves * 32 * blocks); };
+  const int64_t heads = static_cast<int64_t>(batch) * n_kv_heads;
+  plan.blocks = dtype == PRCR_BF16 && rows * stretches(1) * heads >= 1500000 ? 2 : 1;
+  plan.n_stretches = static_cast<int32_t>(stretches(plan.blocks));
+  // The rows are shared out over as many workgroups as run at a time, two on every compute unit, of at
+  // least two tiles each (one prompt of 250 tokens: 15 us in 7 shares, 27 in one), and
+  // those of long runs finer still, because stretches see different numbers of rows (4 prompts of
+  // 2,560: 203 us with 2,048 workgroups, 216 with 1,024, 357 with the 320 of one share).
+  const int64_t have = plan.n_stretches * heads, tiles = rows / (dtype == PRCR_BF16 ? 64 : 32);
+  plan.n_split = static_cast<int32_t>(std::max<int64_t>(
+      {1, std::min<int64_t>(512 / have, tiles / 2), std::min<int64_t>((2048 + have - 1) / have, tiles / 8)}));
   const int64_t elem = dtype == PRCR_F32 ? 4 : 2;
   plan.rotated_bytes = (static_cast<size_t>(total_q) * n_q_heads * head_dim * elem + 255) / 256 * 256;
   plan.bytes = plan.rotated_bytes;

@@ -1,15 +1,15 @@
 // Rotation of query rows, before the keys' weights are summed: every row that counts is
 // turned at its own (t, h, w) position in double precision and rounded once to the stored
-// type, as prefill capture rotates the keys
-// (chunk attention, which reads a row only for its own tile, turns it there).  The matrix products take operands of the
-// stored type, so a query is rounded to it at some point; rounded here, the scores are
-// those of two rows of the same kind, and their sums stay in float32.
+// type, as prefill capture rotates the keys (chunk attention, which reads a row only for
+// its own tile, turns it there).  The matrix products take operands of the stored type, so
+// a query is rounded to it at some point; rounded here, the scores are those of two rows of
+// the same kind, and their sums stay in float32.
 //
 // A thread takes 16 bytes of each half of a token's rows: their angles' cosines and sines
 // once, then the rows of kHeads heads, all read before the first is turned.  What bounds it
-// is reading and writing the rows; of few rows, a thread's own work, and a thread has one head
-// then (32 tokens of 32 heads: 9.1 us with eight heads a thread).  The first workgroup also reports what is wrong
-// with the offsets and lengths, which the kernels after it only skip.
+// is reading and writing the rows (10,240 tokens of 32 heads of 128, 168 MB: 32 us, 5.2 TB/s); of
+// few rows, a thread's own work (32 tokens: 5.0 us).  The first workgroup also reports what
+// is wrong with the offsets and lengths, which the kernels after it only skip.
 #include "attend.h"
 #include "rotary.h"
 
@@ -102,10 +102,14 @@ hipError_t rotate(const AttendParams &in, hipStream_t stream) {
 
 template <typename T>
 hipError_t rotate_dim(const AttendParams &p, int head_dim, hipStream_t stream) {
-  // With a head a thread, fewer than 2^16 threads would be less than a wave on every SIMD.
-  if (static_cast<int64_t>(p.total_q) * p.n_q_heads * (head_dim / 16) < (1 << 19))
-    return head_dim == 64 ? rotate<T, 64, 1>(p, stream) : rotate<T, 128, 1>(p, stream);
-  return head_dim == 64 ? rotate<T, 64, 4>(p, stream) : rotate<T, 128, 4>(p, stream);
+  // bf16 rows in quantity: four heads a thread share the angles (2,560 tokens of 4 sequences: the
+  // keys' weights take 198 us, with one 240); with a head a thread, fewer than 2^16 threads are less
+  // than a wave on every SIMD (48 tokens: 10.9 us with one, 12.3 with four).  float32 rows, whose
+  // turning is double precision throughout, gain nothing (the same 10,240 tokens: 548 and 579 us).
+  if constexpr (sizeof(T) == 2)
+    if (static_cast<int64_t>(p.total_q) * p.n_q_heads * (head_dim / 16) >= (1 << 16))
+      return head_dim == 64 ? rotate<T, 64, 4>(p, stream) : rotate<T, 128, 4>(p, stream);
+  return head_dim == 64 ? rotate<T, 64, 1>(p, stream) : rotate<T, 128, 1>(p, stream);
 }
 
 }  // namespace
