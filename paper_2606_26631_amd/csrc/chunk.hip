@@ -353,11 +353,12 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
 
     // Scores: lane's keys 32 kb + 8 (i / 4) + 4 half + i % 4 of row l32.
     f32x16 s[KB];
-    {
+    [[maybe_unused]] f32x16 lost;              // float32, kFew: of the scores, in their addition
+    const char *const krow = kt + l32 * kRowBytes;
+    const int sw = Tile::key_swizzle(l32);     // (32 rows on, the same)
+    if constexpr (kHalf) {
       // All of the tile's key operands are on their way before the first product waits for one.
       u32x4 k[KB][kQ];
-      const char *const krow = kt + l32 * kRowBytes;
-      const int sw = Tile::key_swizzle(l32);   // (32 rows on, the same)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -369,15 +370,43 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < kQ; ++i) {
-          if constexpr (kHalf) {
-            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[kb][i]),
-                                                            __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
-          } else {
-            const f32x4 a = __builtin_bit_cast(f32x4, k[kb][i]), x = __builtin_bit_cast(f32x4, q[i]);
+        for (int i = 0; i < kQ; ++i)
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[kb][i]),
+                                                          __builtin_bit_cast(bf16x8, q[i]), s[kb], 0, 0, 0);
+      }
+    } else {
+      // In four sums: one sum of D products in a row is off by a unit in the last place of the
+      // score (root mean square), which at scores of 30 and more is 1e-6 of a weight; these, added
+      // up, by 0.4 of that (for 4 % of a call's time).  kFew, whose calls of one token have no other
+      // rows to average over, keeps the additions' errors too: by a quarter (8 % more; without
+      // kFew the registers would not hold them).  The next sum's key operands are on their way
+      // while one is formed.
+      constexpr int kGroup = kQ / 4;
+      u32x4 k[2][kGroup];
+      auto read = [&](int g) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], x[e], s[kb], 0, 0, 0);
-          }
+        for (int i = 0; i < kGroup; ++i)
+          k[g % 2][i] = *reinterpret_cast<const u32x4 *>(krow + ((2 * (g * kGroup + i) + half) ^ sw) * 16);
+      };
+      read(0);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        if (g + 1 < 4) read(g + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 sum;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+          const f32x4 a = __builtin_bit_cast(f32x4, k[g % 2][i]), x = __builtin_bit_cast(f32x4, q[g * kGroup + i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], x[e], sum, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float a = g == 0 ? 0.f : s[0][i], t = a + sum[i], b = t - a;
+          if constexpr (kFew) lost[i] = g == 0 ? 0.f : lost[i] + ((a - (t - b)) + (sum[i] - b));
+          s[0][i] = t;
         }
       }
     }
@@ -417,7 +446,9 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[kb][i] = exp2_hw(fmaf(s[kb][i], p.scale2, -m));
+        float x = fmaf(s[kb][i], p.scale2, -m);
+        if constexpr (!kHalf && kFew) x = fmaf(lost[i] == lost[i] ? lost[i] : 0.f, p.scale2, x);   // (scores that are infinite lose NaN)
+        s[kb][i] = exp2_hw(x);
         if constexpr (kMasked) s[kb][i] = seen(kb, i) ? s[kb][i] : 0.f;
         l += s[kb][i];
       }

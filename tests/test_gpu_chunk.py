@@ -157,6 +157,21 @@ def test_rows_and_keys_shared_out(dtype, H, G, n, past):
     check(out, lse, x.expect())
 
 
+@pytest.mark.parametrize("seed", range(6))
+def test_float32_scores_of_one_token(seed):
+    """One token over 300 slots, scores of some tens: the whole error stays below 1e-6.  (The
+    scores in four sums of 16 products, the sums' errors kept: 0.3 units of 2^-24 x 30 each, and
+    a weight's exponential and the sums' roundings about three of 2^-24.)"""
+    print(f"float32 scores, seed {seed}", flush=True)
+    x = Inputs("f32", 64, 2, 2, [1], [300], seed=seed)
+    x.q, x.k = x.q * 2, x.k * 2
+    out, lse, err = run(x)
+    assert err == 0
+    o, l, _, _, rows = x.expect()
+    got = out.cpu().numpy().astype(np.float64)[rows]
+    assert np.linalg.norm(got - o[rows]) <= 1e-6 * np.linalg.norm(o[rows])
+
+
 def test_padded_rows():
     """A padded [B, S] batch: offsets b S and the rows' counts; padding is left as it is."""
     S, n = 9, np.array([9, 4, 0, 1], np.int32)
