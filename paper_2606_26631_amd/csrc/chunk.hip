@@ -377,10 +377,10 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
     } else {
       // In four sums: one sum of D products in a row is off by a unit in the last place of the
       // score (root mean square), which at scores of 30 and more is 1e-6 of a weight; these, added
-      // up, by 0.4 of that (for 4 % of a call's time).  kFew, whose calls of one token have no other
-      // rows to average over, keeps the additions' errors too: by a quarter (8 % more; without
-      // kFew the registers would not hold them).  The next sum's key operands are on their way
-      // while one is formed.
+      // up, by 0.4 of that (for 4 % of a call's time).  kFew, whose calls of one token have no
+      // other rows to average over, keeps the additions' errors too: by a quarter (300 slots: 15.7
+      // us instead of 13.5; without kFew the registers would not hold them).  The next sum's key
+      // operands are on their way while one is formed.
       constexpr int kGroup = kQ / 4;
       u32x4 k[2][kGroup];
       auto read = [&](int g) {
