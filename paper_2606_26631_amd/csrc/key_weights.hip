@@ -95,20 +95,32 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
                       (chunk ^ (at & (kChunks - 1))) * 16, to + load * 1024);
     }
   };
-  // Of row `threadIdx.x` of a tile: what is taken from its scores (base 2), and the last slot it
-  // sees.  Rows past the last one, and rows that see nothing, give no weight.
+  // Of row `lane` of a tile (every wave has them): its log-sum-exp, and the last slot it sees.
+  constexpr int kPast = INT32_MIN;           // (a row past the last one)
   float lse = 0.f;
-  int limit = 0;
+  int limit = kPast;
   auto load_lse = [&](int r0) {
-    const int r = min(r0 + static_cast<int>(threadIdx.x), n_rows - 1);
-    const int token = token_of(r);
-    limit = first + token;
-    lse = p.lse[row_index(r, token)] * 1.44269504088896341f;
-    if (r0 + static_cast<int>(threadIdx.x) >= n_rows || limit < 0) lse = __builtin_inff();
+    const int r = r0 + lane % kRows, at = min(r, n_rows - 1);
+    const int token = token_of(at);
+    limit = r < n_rows ? first + token : kPast;
+    lse = p.lse[row_index(at, token)];
+  };
+  // What is taken from the rows' scores (base 2), and the last slots, to LDS.  Rows that see no slot,
+  // or have an lse of -infinity, give no weight, whatever their scores are: to the mask they see
+  // none.  Whether there is one, and the tile needs the mask for it.  (Rows past the last one, whose
+  // scores are that one's again, need none: nothing is left of a number less the largest one, and
+  // what is no number, or infinite, has come from the last row already.)
+  auto keep_lse = [&](int to) -> bool {
+    const bool none = limit < 0 || lse == -__builtin_inff();
+    if (threadIdx.x < kRows) {
+      s_lse[to][threadIdx.x] = none ? FLT_MAX : lse * 1.44269504088896341f;
+      s_limit[to][threadIdx.x] = none ? -1 : limit;
+    }
+    return __any(none && limit != kPast);
   };
 
   if (row0 < n_rows) {
-    if (threadIdx.x < kRows) load_lse(row0);
+    load_lse(row0);
     if (kEarly) load_rows(row0, s_rows);
   }
 
@@ -159,20 +171,9 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
   double w[kBlocks] = {};                    // (the first keys add up every row there is: float32 lost 1e-6 of 10,000)
   if (!kEarly && row0 < n_rows) load_rows(row0, s_rows);
   int buf = 0, place = 0;                    // of the present tile, among two and three
-  if (threadIdx.x < kRows) {
-    s_lse[0][threadIdx.x] = lse;
-    s_limit[0][threadIdx.x] = limit;
-  }
-  auto step = [&](int r0, auto is_masked) {
+  bool none = row0 < n_rows && keep_lse(0);  // a row of the present tile gives no weight
+  auto add = [&](auto is_masked) {
     constexpr bool kMasked = decltype(is_masked)::value;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const bool more = r0 + kRows < n_rows;
-    const int next = place == 2 ? 0 : place + 1;
-    if (more) {
-      load_rows(r0 + kRows, s_rows + next * kBytes);
-      if (threadIdx.x < kRows) load_lse(r0 + kRows);
-    }
 #pragma unroll
     for (int rb = 0; rb < kTileBlocks; ++rb) {
       const char *const qrow = s_rows + place * kBytes + (32 * rb + l32) * kRowBytes;
@@ -217,16 +218,25 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
 #pragma unroll
       for (int kb = 0; kb < kBlocks; ++kb) w[kb] += static_cast<double>(sum[kb]);
     }
-    if (more && threadIdx.x < kRows) {
-      s_lse[buf ^ 1][threadIdx.x] = lse;
-      s_limit[buf ^ 1][threadIdx.x] = limit;
+  };
+  for (int r0 = row0; r0 < n_rows; r0 += kRows) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const bool more = r0 + kRows < n_rows;
+    const int next = place == 2 ? 0 : place + 1;
+    if (more) {
+      load_rows(r0 + kRows, s_rows + next * kBytes);
+      load_lse(r0 + kRows);
     }
+    // Rows that all see the whole stretch need no mask.
+    if (none || first + token_of(r0) < k0 + kKeys - 1)
+      add(std::true_type{});
+    else
+      add(std::false_type{});
+    if (more) none = keep_lse(buf ^ 1);
     buf ^= 1;
     place = next;
-  };
-  int r0 = row0;
-  for (; r0 < n_rows && first + token_of(r0) < k0 + kKeys - 1; r0 += kRows) step(r0, std::true_type{});
-  for (; r0 < n_rows; r0 += kRows) step(r0, std::false_type{});   // rows that see the whole stretch
+  }
 #pragma unroll
   for (int kb = 0; kb < kBlocks; ++kb) {
     const float sum = static_cast<float>(w[kb] + __shfl_xor(w[kb], 32));
