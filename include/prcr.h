@@ -385,7 +385,8 @@ prcr_status prcr_decode_attention_static(const prcr_rope *rope, const prcr_cache
  * q_len has no rows (PRCR_DERR_OFFSETS; where q_off decreases, the outputs of the other rows
  * are unspecified); a block-table entry outside the pool skips its keys
  * (PRCR_DERR_BLOCK).  Outputs and workspace must not share memory with an input or
- * with each other (PRCR_ERR_ALIAS).  total_q = 0 is allowed.
+ * with each other (PRCR_ERR_ALIAS).  total_q = 0 is allowed: prcr_chunk_attention, and
+ * prcr_key_weights with accumulate, then launch nothing and report nothing on the device.
  */
 
 /*

@@ -87,6 +87,9 @@ struct WeightsPlan {
 WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
                              int32_t head_dim, int32_t window, prcr_dtype dtype);
 
+// The report that the rotation and chunk attention begin with, by itself: for the keys' weights of a call
+// without rows.
+hipError_t launch_report(const AttendParams &p, hipStream_t stream);
 hipError_t launch_rotate(const AttendParams &p, prcr_dtype dtype, int head_dim, hipStream_t stream);
 hipError_t launch_chunk(const AttendParams &p, const ChunkPlan &plan, prcr_dtype dtype, int head_dim, bool paged,
                         hipStream_t stream);

@@ -238,11 +238,11 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache, prc
   p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.rotated_bytes);
   p.window = window;
   p.accumulate = accumulate != 0;
-  if (total_q > 0) {
-    const prcr_status rotated = launch_status(launch_rotate(p, dtype, rope->head_dim, stream));
-    if (rotated != PRCR_OK) return rotated;
-  } else if (p.accumulate) {
-    return PRCR_OK;                          // no row gives any weight
+  if (total_q == 0 && p.accumulate) return PRCR_OK;   // no row gives any weight
+  if (total_q > 0 || err_flag != nullptr) {
+    const prcr_status first = launch_status(total_q > 0 ? launch_rotate(p, dtype, rope->head_dim, stream)
+                                                        : launch_report(p, stream));
+    if (first != PRCR_OK) return first;
   }
   return launch_status(launch_key_weights(p, plan, dtype, rope->head_dim, cache->paged != 0, stream));
 }

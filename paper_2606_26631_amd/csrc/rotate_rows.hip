@@ -85,6 +85,8 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const AttendParam
   }
 }
 
+__global__ __launch_bounds__(kThreads) void report_kernel(const AttendParams p) { report(p, threadIdx.x, kThreads); }
+
 template <typename T, int D, int kHeads>
 hipError_t rotate(const AttendParams &in, hipStream_t stream) {
   AttendParams p = in;
@@ -113,6 +115,11 @@ hipError_t rotate_dim(const AttendParams &p, int head_dim, hipStream_t stream) {
 }
 
 }  // namespace
+
+hipError_t launch_report(const AttendParams &p, hipStream_t stream) {
+  report_kernel<<<1, kThreads, 0, stream>>>(p);
+  return hipGetLastError();
+}
 
 hipError_t launch_rotate(const AttendParams &p, prcr_dtype dtype, int head_dim, hipStream_t stream) {
   return dtype == PRCR_F32 ? rotate_dim<float>(p, head_dim, stream) : rotate_dim<uint16_t>(p, head_dim, stream);
