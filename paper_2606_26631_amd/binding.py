@@ -232,6 +232,14 @@ def _need(t, name, dtype=None, ndim=None, device=None):
         raise ValueError(f"{name} must have {ndim} dims (got {t.dim()})")
 
 
+def _int32(n, name):
+    """A count or an index as the C interface has it (ctypes would wrap a larger one round)."""
+    n = int(n)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name} {n} does not fit in 32 bits")
+    return n
+
+
 def _dtype_code(t):
     torch = _torch()
     if t.dtype == torch.float32:
@@ -249,7 +257,9 @@ class Rope:
         self.interleaved, self.theta = bool(interleaved), float(theta)
 
     def to_c(self) -> CRope:
-        return CRope(self.head_dim, (c_int32 * 3)(*self.sections), int(self.interleaved), self.theta)
+        return CRope(_int32(self.head_dim, "head_dim"),
+                     (c_int32 * 3)(*(_int32(s, "sections") for s in self.sections)), int(self.interleaved),
+                     self.theta)
 
     def inv_freq(self):
         out = (c_double * (self.head_dim // 2))()
@@ -291,7 +301,7 @@ class Memory:
         self.device = k.device
 
     def to_c(self) -> CMem:
-        B, M, NL, H, D = self.k.shape
+        B, M, NL, H, D = (_int32(n, "mem.k size") for n in self.k.shape)
         return CMem(self.k.data_ptr(), None if self.v is None else self.v.data_ptr(),
                     self.coords.data_ptr(), self.n_visual.data_ptr(), B, M, NL, H, D,
                     _dtype_code(self.k), None if self.v_slot is None else self.v_slot.data_ptr())
@@ -315,10 +325,11 @@ class Cache:
 
     def to_c(self) -> CCache:
         if self.paged:
-            NL, nb, bs, H, D = self.k.shape
+            NL, nb, bs, H, D = (_int32(n, "cache.k size") for n in self.k.shape)
             return CCache(1, self.k.data_ptr(), self.v.data_ptr(), 0, self.block_table.data_ptr(),
-                          bs, self.block_table.shape[1], nb)
-        return CCache(0, self.k.data_ptr(), self.v.data_ptr(), self.k.shape[3], None, 0, 0, 0)
+                          bs, _int32(self.block_table.shape[1], "block_table size"), nb)
+        return CCache(0, self.k.data_ptr(), self.v.data_ptr(), _int32(self.k.shape[3], "cache.k size"),
+                      None, 0, 0, 0)
 
     def check_matches(self, mem: Memory):
         B, M, NL, H, D = mem.k.shape
@@ -339,7 +350,7 @@ def _selection(mem: Memory, sel_off, sel_idx):
     _need(sel_idx, "sel_idx", torch.int32, 1, mem.device)
     if sel_off.shape[0] != mem.k.shape[0] + 1:
         raise ValueError("sel_off must have batch + 1 entries")
-    return int(sel_idx.shape[0])
+    return _int32(sel_idx.shape[0], "sel_idx size")
 
 
 def _overlap(a, b) -> bool:
@@ -375,6 +386,7 @@ def store_raw(mem: Memory, layer: int, raw_k, raw_v, vis_rows, err=None, stream=
     done = (_NATIVE or _native()).store_raw(mem, layer, raw_k, raw_v, vis_rows, err, stream)
     if done is not None:
         return _done("prcr_store_raw", done)
+    layer = _int32(layer, "layer")
     torch = _torch()
     B, M, NL, H, D = mem.k.shape
     _need(raw_k, "raw_k", mem.k.dtype, 4, mem.device)
@@ -388,7 +400,7 @@ def store_raw(mem: Memory, layer: int, raw_k, raw_v, vis_rows, err=None, stream=
     if tuple(vis_rows.shape) != (B, M):
         raise ValueError("vis_rows must be [B, M_max]")
     _err(err, mem.device)
-    st = lib().prcr_store_raw(ctypes.byref(mem.to_c()), int(layer), _ptr(raw_k), _ptr(raw_v),
+    st = lib().prcr_store_raw(ctypes.byref(mem.to_c()), layer, _ptr(raw_k), _ptr(raw_v),
                               int(raw_k.shape[1]), _ptr(vis_rows), _ptr(err),
                               _stream(stream, mem.device))
     _check("prcr_store_raw", st)
@@ -402,6 +414,7 @@ def reassign_coords(mem: Memory, sel_off, sel_idx, p_txt, mode: str = "pcr", l_e
                                                   new_pos, next_pos, err, stream)
     if done is not None:
         return _done("prcr_reassign_coords", done)
+    l_ext = _int32(l_ext, "l_ext")
     torch = _torch()
     total_k = _selection(mem, sel_off, sel_idx)
     B = mem.k.shape[0]
@@ -421,7 +434,7 @@ def reassign_coords(mem: Memory, sel_off, sel_idx, p_txt, mode: str = "pcr", l_e
     if mode not in MODES:
         raise ValueError(f"mode must be one of {sorted(MODES)}")
     st = lib().prcr_reassign_coords(ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx), total_k,
-                                    _ptr(p_txt), MODES[mode], int(l_ext), _ptr(new_pos),
+                                    _ptr(p_txt), MODES[mode], l_ext, _ptr(new_pos),
                                     _ptr(next_pos), _ptr(err), _stream(stream, mem.device))
     _check("prcr_reassign_coords", st)
     return new_pos, next_pos
@@ -473,6 +486,7 @@ def revisit(rope: Rope, mem: Memory, sel_off, sel_idx, p_txt, cache: Cache, cach
                                         store_positions)
     if done is not None:
         return _done("prcr_revisit", done)
+    l_ext = _int32(l_ext, "l_ext")
     torch = _torch()
     total_k = _selection(mem, sel_off, sel_idx)
     B = mem.k.shape[0]
@@ -512,7 +526,7 @@ def revisit(rope: Rope, mem: Memory, sel_off, sel_idx, p_txt, cache: Cache, cach
     if mode not in MODES:
         raise ValueError(f"mode must be one of {sorted(MODES)}")
     st = lib().prcr_revisit(ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off),
-                            _ptr(sel_idx), total_k, _ptr(p_txt), MODES[mode], int(l_ext),
+                            _ptr(sel_idx), total_k, _ptr(p_txt), MODES[mode], l_ext,
                             ctypes.byref(cache.to_c()), _ptr(cache_len), _ptr(new_pos),
                             _ptr(next_pos), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
                             _stream(stream, mem.device))
@@ -528,6 +542,7 @@ def prefill_capture(rope: Rope, mem: Memory, layer: int, raw_k, raw_v, pos, n_to
                                                 cache_start, write_coords, err, stream)
     if done is not None:
         return _done("prcr_prefill_capture", done)
+    layer = _int32(layer, "layer")
     torch = _torch()
     B, M, NL, H, D = mem.k.shape
     cache.check_matches(mem)
@@ -545,7 +560,7 @@ def prefill_capture(rope: Rope, mem: Memory, layer: int, raw_k, raw_v, pos, n_to
     _need(cache_start, "cache_start", torch.int32, 1, mem.device)
     _shape(cache_start, "cache_start", (B,))
     _err(err, mem.device)
-    st = lib().prcr_prefill_capture(ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), int(layer),
+    st = lib().prcr_prefill_capture(ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), layer,
                                     _ptr(raw_k), _ptr(raw_v), int(S), _ptr(pos), _ptr(n_tokens),
                                     _ptr(vis_index), int(bool(write_coords)),
                                     ctypes.byref(cache.to_c()), _ptr(cache_start), _ptr(err),
@@ -567,8 +582,8 @@ def decode_workspace_bytes(cache: Cache, batch: int, n_q_heads: int) -> int:
     NL, H, D = _cache_dims(cache)
     out = ctypes.c_size_t(0)
     _check("prcr_decode_workspace_size",
-           lib().prcr_decode_workspace_size(ctypes.byref(cache.to_c()), int(batch), int(n_q_heads),
-                                            int(H), int(D), ctypes.byref(out)))
+           lib().prcr_decode_workspace_size(ctypes.byref(cache.to_c()), _int32(batch, "batch"),
+                                            _int32(n_q_heads, "n_q_heads"), int(H), int(D), ctypes.byref(out)))
     return int(out.value)
 
 
@@ -580,6 +595,7 @@ def decode_attention(rope: Rope, cache: Cache, layer: int, q, q_pos, cache_len, 
                                                  workspace, err, stream)
     if done is not None:
         return _done("prcr_decode_attention", done)
+    layer = _int32(layer, "layer")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     _need(q, "q", cache.k.dtype, 3, cache.device)
@@ -607,7 +623,7 @@ def decode_attention(rope: Rope, cache: Cache, layer: int, q, q_pos, cache_len, 
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
     st = lib().prcr_decode_attention(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
-                                     _dtype_code(cache.k), int(B), int(NL), int(H), int(layer),
+                                     _dtype_code(cache.k), int(B), int(NL), int(H), layer,
                                      _ptr(q), int(Hq), _ptr(q_pos), _ptr(cache_len), sc, _ptr(out),
                                      _ptr(workspace), workspace.numel() * workspace.element_size(),
                                      _ptr(err), _stream(stream, cache.device))
@@ -625,6 +641,7 @@ def decode_attention_static(rope: Rope, cache: Cache, layer: int, q, q_pos, cach
                                                         out, err, stream)
     if done is not None:
         return _done("prcr_decode_attention_static", done)
+    layer = _int32(layer, "layer")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     _need(q, "q", cache.k.dtype, 3, cache.device)
@@ -647,7 +664,7 @@ def decode_attention_static(rope: Rope, cache: Cache, layer: int, q, q_pos, cach
     sc = float(D) ** -0.5 if scale is None else float(scale)
     st = lib().prcr_decode_attention_static(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
                                             _dtype_code(cache.k), int(B), int(NL), int(H),
-                                            int(layer), _ptr(q), int(Hq), _ptr(q_pos),
+                                            layer, _ptr(q), int(Hq), _ptr(q_pos),
                                             _ptr(cache_len), sc, _ptr(out), _ptr(err),
                                             _stream(stream, cache.device))
     _check("prcr_decode_attention_static", st)
@@ -703,8 +720,8 @@ def _query_rows(cache: Cache, q, q_off, q_pos, cache_len, q_len):
 def chunk_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int) -> int:
     """Bytes of workspace prcr_chunk_attention needs (prcr_chunk_workspace_size)."""
     NL, H, D = _cache_dims(cache)
-    return _size_t("prcr_chunk_workspace_size", ctypes.byref(cache.to_c()), _batch(cache), int(total_q),
-                   int(n_q_heads), int(H), int(D))
+    return _size_t("prcr_chunk_workspace_size", ctypes.byref(cache.to_c()), _batch(cache),
+                   _int32(total_q, "total_q"), _int32(n_q_heads, "n_q_heads"), int(H), int(D))
 
 
 def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len, q_len=None,
@@ -718,6 +735,7 @@ def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache
                                                   scale, out, lse, workspace, err, stream)
     if done is not None:
         return _done("prcr_chunk_attention", done)
+    layer = _int32(layer, "layer")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B, T, Hq = _query_rows(cache, q, q_off, q_pos, cache_len, q_len)
@@ -734,7 +752,7 @@ def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache
     sc = float(D) ** -0.5 if scale is None else float(scale)
     st = lib().prcr_chunk_attention(
         ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H),
-        int(layer), _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len), sc,
+        layer, _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len), sc,
         _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err),
         _stream(stream, cache.device))
     _check("prcr_chunk_attention", st)
@@ -745,8 +763,8 @@ def key_weights_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int, wind
     """Bytes of workspace prcr_key_weights needs (prcr_key_weights_workspace_size)."""
     NL, H, D = _cache_dims(cache)
     return _size_t("prcr_key_weights_workspace_size", ctypes.byref(cache.to_c()), _dtype_code(cache.k),
-                   _batch(cache), int(total_q), int(n_q_heads), int(H), int(D),
-                   0 if window is None else int(window))
+                   _batch(cache), _int32(total_q, "total_q"), _int32(n_q_heads, "n_q_heads"), int(H), int(D),
+                   0 if window is None else _int32(window, "window"))
 
 
 def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len, lse, q_len=None,
@@ -759,12 +777,14 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
                                               window, scale, weights, accumulate, workspace, err, stream)
     if done is not None:
         return _done("prcr_key_weights", done)
+    layer = _int32(layer, "layer")
+    window = None if window is None else _int32(window, "window")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B, T, Hq = _query_rows(cache, q, q_off, q_pos, cache_len, q_len)
     _need(lse, "lse", torch.float32, 2, cache.device)
     _shape(lse, "lse", (T, Hq))
-    if window is not None and int(window) < 1:
+    if window is not None and window < 1:
         raise ValueError("window must be at least 1 (None: all rows)")
     if weights is None:
         if accumulate:
@@ -777,8 +797,8 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
     sc = float(D) ** -0.5 if scale is None else float(scale)
     st = lib().prcr_key_weights(
         ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H),
-        int(layer), _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len),
-        _ptr(lse), 0 if window is None else int(window), sc, int(bool(accumulate)), _ptr(weights),
+        layer, _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len),
+        _ptr(lse), 0 if window is None else window, sc, int(bool(accumulate)), _ptr(weights),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err),
         _stream(stream, cache.device))
     _check("prcr_key_weights", st)
@@ -787,7 +807,7 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
 
 def evict_workspace_bytes(cache: Cache, budget: int) -> int:
     """Bytes of workspace prcr_evict needs (prcr_evict_workspace_size)."""
-    return _size_t("prcr_evict_workspace_size", ctypes.byref(cache.to_c()), _batch(cache), int(budget))
+    return _size_t("prcr_evict_workspace_size", ctypes.byref(cache.to_c()), _batch(cache), _int32(budget, "budget"))
 
 
 def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, keep_last: int = 0, mem=None,
@@ -801,10 +821,11 @@ def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, ke
                                         new_cache_len, kept, new_weights, workspace, err, stream)
     if done is not None:
         return _done("prcr_evict", done)
+    budget, keep_first, keep_last = (_int32(budget, "budget"), _int32(keep_first, "keep_first"),
+                                     _int32(keep_last, "keep_last"))
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B, cap = _batch(cache), _capacity(cache)
-    budget = int(budget)
     _need(cache_len, "cache_len", torch.int32, 1, cache.device)
     _shape(cache_len, "cache_len", (B,))
     _need(weights, "weights", torch.float32, 3, cache.device)
@@ -829,7 +850,7 @@ def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, ke
     _err(err, cache.device)
     st = lib().prcr_evict(
         ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H), int(D), _ptr(cache_len),
-        _ptr(weights), budget, int(keep_first), int(keep_last), _ptr(new_cache_len), _ptr(kept),
+        _ptr(weights), budget, keep_first, keep_last, _ptr(new_cache_len), _ptr(kept),
         _ptr(new_weights), None if mem is None else ctypes.byref(mem.to_c()), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
     _check("prcr_evict", st)
