@@ -413,7 +413,9 @@ prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,
                                  size_t workspace_bytes, int32_t *err_flag,
                                  hipStream_t stream);
 
-/* Workspace bytes prcr_chunk_attention needs for this cache and shape (host). */
+/* Workspace bytes prcr_chunk_attention needs for this cache and shape (host).  Another shape may
+ * need more, one of fewer rows too (their keys are shared out finer): a program whose shapes
+ * change asks for each, or has 2^18 (head_dim + 2) bytes, more than which no shape needs. */
 prcr_status prcr_chunk_workspace_size(const prcr_cache *cache, int32_t batch,
                                       int32_t total_q, int32_t n_q_heads,
                                       int32_t n_kv_heads, int32_t head_dim, size_t *bytes);
@@ -444,7 +446,9 @@ prcr_status prcr_key_weights(const prcr_rope *rope, const prcr_cache *cache,
                              void *workspace, size_t workspace_bytes, int32_t *err_flag,
                              hipStream_t stream);
 
-/* Workspace bytes prcr_key_weights needs for this cache, shape and window (host). */
+/* Workspace bytes prcr_key_weights needs for this cache, shape and window (host); those of
+ * another shape as with chunk attention.  No shape needs more than 2^22 bytes beyond its rotated
+ * rows: total_q n_q_heads head_dim elements of dtype, rounded up to 256 bytes. */
 prcr_status prcr_key_weights_workspace_size(const prcr_cache *cache, prcr_dtype dtype,
                                             int32_t batch, int32_t total_q,
                                             int32_t n_q_heads, int32_t n_kv_heads,

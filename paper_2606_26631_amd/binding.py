@@ -718,7 +718,8 @@ def _query_rows(cache: Cache, q, q_off, q_pos, cache_len, q_len):
 
 
 def chunk_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int) -> int:
-    """Bytes of workspace prcr_chunk_attention needs (prcr_chunk_workspace_size)."""
+    """Bytes of workspace prcr_chunk_attention needs for these very numbers; fewer rows may need more
+    (prcr_chunk_workspace_size, which also gives a bound for all)."""
     NL, H, D = _cache_dims(cache)
     return _size_t("prcr_chunk_workspace_size", ctypes.byref(cache.to_c()), _batch(cache),
                    _int32(total_q, "total_q"), _int32(n_q_heads, "n_q_heads"), int(H), int(D))
@@ -760,7 +761,8 @@ def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache
 
 
 def key_weights_workspace_bytes(cache: Cache, total_q: int, n_q_heads: int, window=None) -> int:
-    """Bytes of workspace prcr_key_weights needs (prcr_key_weights_workspace_size)."""
+    """Bytes of workspace prcr_key_weights needs for these very numbers; fewer rows may need more
+    (prcr_key_weights_workspace_size, which also gives a bound for all)."""
     NL, H, D = _cache_dims(cache)
     return _size_t("prcr_key_weights_workspace_size", ctypes.byref(cache.to_c()), _dtype_code(cache.k),
                    _batch(cache), _int32(total_q, "total_q"), _int32(n_q_heads, "n_q_heads"), int(H), int(D),

@@ -785,6 +785,7 @@ ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n
   const double best = rounds <= 2 ? 1 : std::sqrt(rounds * (plan.few ? 16e6 : 4e6) / (rows_all * 8 * (head_dim + 2)));
   const int64_t most = std::min<int64_t>({(plan.few ? 256 : 512) / have, (capacity + keys - 1) / keys, kMostSplits});
   plan.n_split = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most, static_cast<int64_t>(best))));
+  // (Of several splits there are at most 512 workgroups, so partial results of at most 512 x 128 rows.)
   if (plan.n_split > 1) plan.bytes = static_cast<size_t>(total_q) * n_q_heads * plan.n_split * (head_dim + 2) * 4;
   return plan;
 }

@@ -330,6 +330,7 @@ WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, i
   const int64_t elem = dtype == PRCR_F32 ? 4 : 2;
   plan.rotated_bytes = (static_cast<size_t>(total_q) * n_q_heads * head_dim * elem + 255) / 256 * 256;
   plan.bytes = plan.rotated_bytes;
+  // (Of several shares there are less than 4,096 workgroups, so partial sums of 4,096 x 256 keys at most.)
   if (plan.n_split > 1) plan.bytes += static_cast<size_t>(plan.n_split) * batch * n_kv_heads * capacity * 4;
   return plan;
 }
