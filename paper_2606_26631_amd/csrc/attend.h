@@ -41,9 +41,8 @@ struct AttendParams {
                                   // weights: key stretches of a sequence, row splits (launcher)
   int32_t window;                 // weights: the last rows of each sequence that count (0: all)
   int32_t accumulate;
-  float scale;                    // |scale|; a negative one turns the rotated queries' sign
   float scale2;                   // |scale| log2(e)
-  int32_t negate;
+  int32_t negate;                 // a negative scale: the rotated queries' sign is turned
   Divisor by_group, by_heads, by_split, by_slot, by_row;
   int8_t axis[kMaxPairs];
   double inv_freq[kMaxPairs];

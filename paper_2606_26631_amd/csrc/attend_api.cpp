@@ -129,7 +129,6 @@ prcr_status prepare(const prcr_rope *rope, const prcr_cache *cache, prcr_dtype d
       if ((1 << s) == cache->block_size) p.block_shift = s;
   p.capacity = static_cast<int32_t>(capacity);
   p.negate = scale < 0.f;
-  p.scale = std::fabs(scale);
   p.scale2 = static_cast<float>(std::fabs(static_cast<double>(scale)) * 1.4426950408889634);
   p.by_group = Divisor::of(p.group);
   p.by_heads = Divisor::of(n_kv_heads);
