@@ -8,8 +8,8 @@
 // rows, 32 for all its waves; the rows of a KV head are its tokens' query heads, token by
 // token, so that a tile reads the cache once for all heads of the group.  Tiles of keys and
 // values go through LDS, two of them, the next one's loads in flight while the present one is
-// used: a tile of 64 keys is used by 128 rows, so that LDS is filled at a sixth of what it
-// is read at, and two workgroups with their 128 registers a lane fit a compute unit.  The wave forms the scores
+// used: a tile of 64 keys is used by 128 rows, so that LDS is filled at a quarter of what it
+// is read at, and two workgroups, of up to 256 registers a lane, fit a compute unit.  The wave forms the scores
 // transposed, K (32 keys) x Q^T (32 rows): a lane then holds scores of one row only (that
 // of its product column), the running maximum and sum of the softmax are one register
 // each, and the weights are, in the registers where they arise, the operand of the value
@@ -380,8 +380,11 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
       // up, by 0.4 of that (for 4 % of a call's time).  kFew, whose calls of one token have no
       // other rows to average over, keeps the additions' errors too: by a quarter (300 slots: 15.7
       // us instead of 13.5; without kFew the registers would not hold them).  The next sum's key
-      // operands are on their way while one is formed.
+      // operands are on their way while one is formed, but for paged rows of 128 in quantity: there the
+      // registers they take would spill (4 prompts of 1,500 tokens, 8 heads of 4: 692 us without, 693
+      // with them; 400 tokens each on some 1,500 cached ones, blocks of 5: 445 and 448).
       constexpr int kGroup = kQ / 4;
+      constexpr bool kAhead = D == 64 || !kPaged || kFew;
       u32x4 k[2][kGroup];
       auto read = [&](int g) {
 #pragma unroll
@@ -391,7 +394,8 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
       read(0);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        if (g + 1 < 4) read(g + 1);
+        if (!kAhead && g > 0) read(g);
+        if (kAhead && g + 1 < 4) read(g + 1);
         __builtin_amdgcn_sched_barrier(0);
         f32x16 sum;
 #pragma unroll
