@@ -401,6 +401,7 @@ prcr_status prcr_decode_attention_static(const prcr_rope *rope, const prcr_cache
  * bfloat16 for the product with the values (their sum is taken before that), and out is rounded once.  A row
  * that sees no slot gets out = 0 and lse = -infinity.  Values and keys at slots that a row
  * does not see have no influence on it, whatever they are; a NaN at one that it sees makes it NaN.
+ * Keys that score -infinity have no weight, and a row that sees no others is like one that sees none.
  * Rows of no sequence (padding, rows behind the last sequence) are left as they were.
  */
 prcr_status prcr_chunk_attention(const prcr_rope *rope, const prcr_cache *cache,

@@ -38,7 +38,7 @@ __device__ __forceinline__ void load_to_lds(const char *from, char *to) {
 // a sequence per lane (every round costs about a microsecond before the first key), and
 // their tiles are counted: tile slots are one behind the other, the workgroups without one at the end.
 // Between the others, such workgroups left dies idle: 64 sequences of 32 rows, every second slot
-// empty, took 137 us (float32, 1,160 slots) and now take 80.  Of more sequences, sequence b has the slots from
+// empty, took 137 us (float32, 1,160 slots), and 80 so (now, with the scores in four sums, 90).  Of more sequences, sequence b has the slots from
 // floor(q_off[b] G / M) + b on, enough of them for its rows' tiles of M.
 struct Sequence {
   int b, tile;                               // and the workgroup's tile of its rows (none: below 0)
@@ -463,7 +463,10 @@ __global__ __launch_bounds__(kThreads, kFew ? 1 : 2) void chunk_kernel(const Att
     bool odd = false;
     if constexpr (kHalf) {
       // A lane's weights of 16 keys (step c) are keys 16 c + 4 half + 0..3 and 8 further on; the
-      // transposing read gives it feature l32's values of the same ones.
+      // transposing read gives it feature l32's values of the same ones.  The products take bf16: a
+      // weight is rounded to it here, after it has gone into the sum.  Outputs are then off by 2.1 to 2.3
+      // thousandths of their norm, of which rounding them alone makes 1.6; the rest would take a second
+      // part of the weights, and half as many products again.
       u32x4 w[2 * KB];
 #pragma unroll
       for (int c = 0; c < 2 * KB; ++c)
@@ -769,8 +772,8 @@ ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n
   auto tiles = [&](int64_t m) { return std::max<int64_t>(batch * ((rows + m * batch - 1) / (m * batch)) * n_kv_heads, 1); };
   // Tiles of 32 rows whose keys the waves share out take a compute unit each (their LDS): where
   // one round of them does it.  bf16, 8 KV heads of 4 query heads, 4,000 cached slots, both ways:
-  // one sequence of 40 rows, 40 workgroups, 18 and 30 us; 16 sequences of 16, 256 workgroups, 50
-  // and 56; 4 sequences of 120, 480 workgroups, 82 and 66.
+  // one sequence of 40 rows, 40 workgroups, 18 and 21 us; 16 sequences of 16, 256 workgroups, 52
+  // and 58; 4 sequences of 120, 480 workgroups, 73 and 59.
   plan.few = tiles(32) <= 256;
   const int64_t tile = plan.few ? 32 : 32 * kWaves, have = tiles(tile);
   plan.n_slots = static_cast<int32_t>(rows / tile) + batch;
@@ -778,12 +781,13 @@ ChunkPlan plan_chunk(int64_t capacity, int32_t batch, int32_t total_q, int32_t n
   // compute unit, else two), or, of fewer, by what that costs: a workgroup takes about a
   // microsecond for 64 keys (of each wave, where they share them out), and every split
   // writes and reads a partial result of 4 (D + 2) bytes per row and head, at some 16 MB a
-  // microsecond, or 4 MB where a workgroup writes those of 128 rows at its end (one sequence
-  // of 40 rows over 1,192 slots: 13.4 us with 16, 14.9 with 4; of 400 rows over 500 slots: 21 us
-  // with 4, 27 with 16; over 1,552 slots 35 with 4, 36 with 16, 41 with 1).  The merge is
+  // microsecond, or 4 MB where a workgroup writes those of 128 rows at its end (of bf16 and the heads
+  // above, one sequence of 40 rows over 1,192 slots: 13.0 us in 5 splits, 16.3 in 2; of 400 rows over
+  // 500 slots: 21 us in one, 26 in 4; over 1,552 slots: 39 in one, 33 in 2, 34 in 4, 73 in 16).  The merge is
   // a launch more, about four microseconds: two rounds or fewer are not split.  A round that is
   // not full is better than two: one sequence of 400 rows over 4,400 slots, 104 workgroups, takes
-  // 61 us in 4 splits, 70 in 5.  (The lengths are on the device: the capacity stands for them.)
+  // 55 us in 4 splits, 66 in 5.  (The lengths are on the device: the capacity stands for them.  Float32,
+  // whose tiles are of 32 keys and take longer, goes by the same rule, which was not measured for it.)
   const int64_t keys = plan.few ? 64 * kWaves : 64;          // of a workgroup at a time
   const double rounds = static_cast<double>(capacity) / keys, rows_all = static_cast<double>(total_q) * n_q_heads;
   const double best = rounds <= 2 ? 1 : std::sqrt(rounds * (plan.few ? 16e6 : 4e6) / (rows_all * 8 * (head_dim + 2)));

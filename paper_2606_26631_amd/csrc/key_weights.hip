@@ -12,8 +12,9 @@
 // kernel adds in order.
 //
 // What bounds it: of few rows, reading the keys (one token of 32 sequences of 3,500 slots, 8 heads of
-// 128: 230 MB in 50 us, 4.6 TB/s); of many, an exponential and a sum per score beside the products
-// (4 prompts of 2,560 tokens, 32 heads: 147 us, 0.73 PF of products).
+// 128: 230 MB in 45 us, 5.1 TB/s); of many, an exponential and a sum per score beside the products
+// (4 prompts of 2,560 tokens, 32 heads: 160 us, 0.67 PF of products).  In between, a workgroup's start
+// counts: it waits for its stretch of keys before the first product, and has few row tiles for them.
 #include <algorithm>
 #include <type_traits>
 
@@ -210,6 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void key_weights_kernel(const AttendPa
           const int last = kMasked ? s_limit[buf][at + e] : 0;
 #pragma unroll
           for (int kb = 0; kb < kBlocks; ++kb) {
+            // (The factor log2 e is in scale2 and in off, in each with a rounding of its own.)
             const float x = exp2_hw(fmaf(s[kb][4 * i + e], p.scale2, -off[e]));
             sum[kb] += !kMasked || kw + 32 * kb + l32 <= last ? x : 0.f;
           }
@@ -313,17 +315,19 @@ WeightsPlan plan_key_weights(int64_t capacity, int32_t batch, int32_t total_q, i
   const int64_t rows = tokens * (n_q_heads / n_kv_heads);     // of a sequence and KV head, on average
   // Two key blocks a wave use a row tile's read for both, but make half as many workgroups: for
   // long runs, counted as rows times stretches of 128 keys.  bf16, 8 KV heads of 4 query heads:
-  // 4 prompts of 2,560 tokens (6.6 million) take 203 us with two and 211 with one; one
-  // prompt of 1,000 (0.3 million) 39 and 34; 250 tokens over 1,400 slots of 16 sequences
-  // (1.4 million) 95 and 96.  (float32, whose keys would take 256 registers, has one.)
+  // 4 prompts of 2,560 tokens (6.6 million) take 185 us with two and 194 with one; one
+  // prompt of 1,000 (0.3 million) 31 and 27; 250 tokens over 1,400 slots of 16 sequences
+  // (1.4 million) 83 and 88.  (float32, whose keys would take 256 registers, has one.)
   auto stretches = [&](int64_t blocks) { return (capacity + kWaves * 32 * blocks - 1) / (kWaves * 32 * blocks); };
   const int64_t heads = static_cast<int64_t>(batch) * n_kv_heads;
   plan.blocks = dtype == PRCR_BF16 && rows * stretches(1) * heads >= 1500000 ? 2 : 1;
   plan.n_stretches = static_cast<int32_t>(stretches(plan.blocks));
   // The rows are shared out over as many workgroups as run at a time, two on every compute unit, of at
-  // least two tiles each (one prompt of 250 tokens: 15 us in 7 shares, 27 in one), and
+  // least two tiles each (one prompt of 250 tokens: 14.4 us in 7 shares, 27 in one), and
   // those of long runs finer still, because stretches see different numbers of rows (4 prompts of
-  // 2,560: 203 us with 2,048 workgroups, 216 with 1,024, 357 with the 320 of one share).
+  // 2,560, 352 stretches: 185 us in 6 shares, 200 in 4, 218 in 3, 413 in one).  Stretches behind a
+  // sequence's length are counted too, since the lengths are on the device: with a capacity of 8,192 slots
+  // those prompts take 296 us (2 shares), with 32,768 446 (one).
   const int64_t have = plan.n_stretches * heads, tiles = rows / (dtype == PRCR_BF16 ? 64 : 32);
   plan.n_split = static_cast<int32_t>(std::max<int64_t>(
       {1, std::min<int64_t>(512 / have, tiles / 2), std::min<int64_t>((2048 + have - 1) / have, tiles / 8)}));

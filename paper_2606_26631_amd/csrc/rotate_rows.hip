@@ -105,9 +105,9 @@ hipError_t rotate(const AttendParams &in, hipStream_t stream) {
 template <typename T>
 hipError_t rotate_dim(const AttendParams &p, int head_dim, hipStream_t stream) {
   // bf16 rows in quantity: four heads a thread share the angles (2,560 tokens of 4 sequences: the
-  // keys' weights take 198 us, with one 240); with a head a thread, fewer than 2^16 threads are less
-  // than a wave on every SIMD (48 tokens: 10.9 us with one, 12.3 with four).  float32 rows, whose
-  // turning is double precision throughout, gain nothing (the same 10,240 tokens: 548 and 579 us).
+  // keys' weights take 185 us, with one 221); with a head a thread, fewer than 2^16 threads are less
+  // than a wave on every SIMD (48 tokens: 10.4 us with one, 11.6 with four).  float32 rows, whose
+  // turning is double precision throughout, gain nothing (the same 10,240 tokens: 1,056 and 1,058 us).
   if constexpr (sizeof(T) == 2)
     if (static_cast<int64_t>(p.total_q) * p.n_q_heads * (head_dim / 16) >= (1 << 16))
       return head_dim == 64 ? rotate<T, 64, 4>(p, stream) : rotate<T, 128, 4>(p, stream);
