@@ -495,6 +495,99 @@ prcr_status prcr_evict(const prcr_cache *cache, prcr_dtype dtype, int32_t batch,
 prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch,
                                       int32_t budget, size_t *bytes);
 
+/*
+ * The decoder cache in 8 bits.  A row (one slot, layer and KV head) is head_dim codes of a byte each
+ * and a float32 scale; it stands for code_i scale.  With x the row that a cache of dtype would
+ * hold (keys turned in double precision and rounded once, as prcr_prefill_capture writes them,
+ * values as they are) and Q the largest code, 448 or 127, all in float32:
+ *   scale = max(max |x_i| / Q, 2^-126),   code_i = nearest(x_i (1 / scale)), ties to even
+ * so that code_i scale is within 2^-4 of x_i relative to it or 2^-10 scale (E4M3), or within scale / 2
+ * (I8), each but for float32's roundings.  A row with an infinity or a NaN gets codes 0 and scale NaN: all of it reads back
+ * as NaN.
+ *
+ * Every array that a call writes must share no memory with another one (PRCR_ERR_ALIAS).  head_dim 64 or 128 and the
+ * axis maps of prcr_rebind_inject; the capacity per sequence (s_max, or max_blocks * block_size) at
+ * most 2^30 slots, batch and n_kv_heads at most 65535, else PRCR_ERR_SHAPE.
+ */
+typedef enum prcr_code PRCR_ENUM_BASE {
+  PRCR_E4M3 = 0,               /* 8-bit float, 4 exponent and 3 fraction bits, no infinities */
+  PRCR_I8 = 1                  /* integers -127 .. 127                                       */
+} prcr_code;
+
+typedef struct prcr_quant_cache {
+  prcr_cache cache;            /* k, v: the codes; layouts and geometry as there             */
+  float *k_scale;              /* contiguous [batch][n_layers][n_kv_heads][s_max]            */
+  float *v_scale;              /* paged [n_layers][n_blocks][n_kv_heads][block_size]         */
+  prcr_code code;
+} prcr_quant_cache;
+
+/*
+ * prcr_quant_append - tokens of one layer appended to the cache in 8 bits: a prompt's, a turn's, or a
+ * decoded token's keys and values as the layer makes them.
+ *
+ *   raw_k, raw_v  [batch][s_src][n_kv_heads][head_dim], dtype, before rotary
+ *   pos           int32 [batch][s_src][3]: (t, h, w) position ids of each row
+ *   n_tokens      int32 [batch]: rows s < n_tokens[b] are tokens
+ *   cache_start   int32 [batch]: row s goes to slot cache_start[b] + s of layer `layer`
+ * batch * s_src at most 2^31 - 1.  n_tokens[b] outside [0, s_src] raises PRCR_DERR_INDEX (negative: no
+ * tokens; more: s_src); a slot beyond the capacity or a bad block skips the token
+ * (PRCR_DERR_CAPACITY / _BLOCK).  (The memory of raw rows is filled by prcr_store_raw.)
+ */
+prcr_status prcr_quant_append(const prcr_rope *rope, const prcr_quant_cache *cache,
+                              prcr_dtype dtype, int32_t batch, int32_t n_layers,
+                              int32_t n_kv_heads, int32_t layer, const void *raw_k,
+                              const void *raw_v, int32_t s_src, const int32_t *pos,
+                              const int32_t *n_tokens, const int32_t *cache_start,
+                              int32_t *err_flag, hipStream_t stream);
+
+/*
+ * prcr_quant_rebind_inject - prcr_rebind_inject into a cache in 8 bits: arguments, outputs and errors are
+ * those of prcr_rebind_inject.  Keys are turned at new_pos and rounded to mem->dtype before they are
+ * quantised, so that a token revisited at the position it was appended at has the same codes.
+ * A position beyond 2^50 in magnitude gives unspecified codes.  With
+ * a key-only memory the value's codes and scale are copied from slot v_slot[b][m] of the cache.
+ */
+prcr_status prcr_quant_rebind_inject(const prcr_rope *rope, const prcr_mem *mem,
+                                     const int32_t *sel_off, const int32_t *sel_idx,
+                                     int32_t total_k, const double *new_pos,
+                                     const prcr_quant_cache *cache, const int32_t *cache_len,
+                                     int32_t *new_cache_len, int64_t *slot_mapping,
+                                     int32_t *err_flag, hipStream_t stream);
+
+/*
+ * prcr_quant_read - one layer read back into rows of dtype: slots below cache_len[b] of every
+ * sequence and KV head, code_i scale in float32 rounded once to dtype.
+ *
+ *   k, v          out [batch][1][n_kv_heads][s_out][head_dim], 16-byte aligned: a contiguous cache of
+ *                 one layer, which prcr_chunk_attention and prcr_key_weights take
+ * Slots from cache_len[b] on are left as they were.  A cache_len beyond the capacity, or beyond s_out, is
+ * clamped with PRCR_DERR_CAPACITY; a bad block skips its slots (PRCR_DERR_BLOCK).
+ */
+prcr_status prcr_quant_read(const prcr_quant_cache *cache, prcr_dtype dtype, int32_t batch,
+                            int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                            int32_t layer, const int32_t *cache_len, void *k, void *v,
+                            int32_t s_out, int32_t *err_flag, hipStream_t stream);
+
+/*
+ * prcr_quant_decode_attention - prcr_decode_attention over a cache in 8 bits, whose rows stand for
+ * code_i scale: arguments, results and errors are those of prcr_decode_attention, dtype being that
+ * of q.  The query is turned in double precision and rounded to float32 once; scores, the softmax
+ * and the sums are float32, and the codes enter the products exactly.
+ * The workspace has prcr_quant_decode_workspace_size() bytes.
+ */
+prcr_status prcr_quant_decode_attention(const prcr_rope *rope, const prcr_quant_cache *cache,
+                                        prcr_dtype dtype, int32_t batch, int32_t n_layers,
+                                        int32_t n_kv_heads, int32_t layer, const void *q,
+                                        int32_t n_q_heads, const int32_t *q_pos,
+                                        const int32_t *cache_len, float scale, float *out,
+                                        void *workspace, size_t workspace_bytes,
+                                        int32_t *err_flag, hipStream_t stream);
+
+/* Workspace bytes prcr_quant_decode_attention needs for this cache and shape (host). */
+prcr_status prcr_quant_decode_workspace_size(const prcr_quant_cache *cache, int32_t batch,
+                                             int32_t n_q_heads, int32_t n_kv_heads,
+                                             int32_t head_dim, size_t *bytes);
+
 /* Host helpers (no GPU work). */
 
 /* Static description of a status code (host). */

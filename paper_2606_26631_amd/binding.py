@@ -26,6 +26,7 @@ from ctypes import POINTER, c_double, c_int, c_int32, c_void_p
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libprcr.so")
 
 PRCR_F32, PRCR_BF16 = 0, 1
+PRCR_E4M3, PRCR_I8 = 0, 1
 MODES = {"pcr": 0, "shift": 1, "identity": 2, "lpa": 3, "uir": 4, "pcr_right": 5}
 DERR_INDEX, DERR_CAPACITY, DERR_BLOCK, DERR_OFFSETS, DERR_RANGE = 1, 2, 4, 8, 16
 STATUS = {0: "PRCR_OK", 1: "PRCR_ERR_NULL", 2: "PRCR_ERR_SHAPE", 3: "PRCR_ERR_DTYPE",
@@ -56,6 +57,10 @@ class CCache(ctypes.Structure):
     _fields_ = [("paged", c_int32), ("k", c_void_p), ("v", c_void_p), ("s_max", c_int32),
                 ("block_table", c_void_p), ("block_size", c_int32), ("max_blocks", c_int32),
                 ("n_blocks", c_int32)]
+
+
+class CQuantCache(ctypes.Structure):
+    _fields_ = [("cache", CCache), ("k_scale", c_void_p), ("v_scale", c_void_p), ("code", c_int)]
 
 
 _LIB = None
@@ -132,6 +137,25 @@ def lib() -> ctypes.CDLL:
     L.prcr_evict.argtypes = [POINTER(CCache), c_int, c_int32, c_int32, c_int32, c_int32, c_void_p,
                              c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
                              POINTER(CMem), c_void_p, ctypes.c_size_t, c_void_p, c_void_p]
+    L.prcr_quant_append.restype = c_int
+    L.prcr_quant_append.argtypes = [POINTER(CRope), POINTER(CQuantCache), c_int, c_int32, c_int32, c_int32,
+                                    c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_void_p]
+    L.prcr_quant_rebind_inject.restype = c_int
+    L.prcr_quant_rebind_inject.argtypes = [POINTER(CRope), POINTER(CMem), c_void_p, c_void_p, c_int32,
+                                           c_void_p, POINTER(CQuantCache), c_void_p, c_void_p, c_void_p,
+                                           c_void_p, c_void_p]
+    L.prcr_quant_read.restype = c_int
+    L.prcr_quant_read.argtypes = [POINTER(CQuantCache), c_int, c_int32, c_int32, c_int32, c_int32, c_int32,
+                                  c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]
+    L.prcr_quant_decode_workspace_size.restype = c_int
+    L.prcr_quant_decode_workspace_size.argtypes = [POINTER(CQuantCache), c_int32, c_int32, c_int32, c_int32,
+                                                   POINTER(ctypes.c_size_t)]
+    L.prcr_quant_decode_attention.restype = c_int
+    L.prcr_quant_decode_attention.argtypes = [POINTER(CRope), POINTER(CQuantCache), c_int, c_int32, c_int32,
+                                              c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                              ctypes.c_float, c_void_p, c_void_p, ctypes.c_size_t, c_void_p,
+                                              c_void_p]
     _LIB = L
     return L
 
@@ -157,7 +181,7 @@ def _native():
             built_for = getattr(module, "built_for", "an earlier version")
             if built_for != here:
                 raise ImportError(f"it was built for {built_for}, this is {here}")
-            module.setup(Rope, Memory, Cache, MODES)
+            module.setup(Rope, Memory, Cache, MODES, QuantCache)
         except ImportError as e:
             warnings.warn(f"the native module of the entry points is not used ({e}): every call costs some "
                           "20 us more of host time; paper_2606_26631_amd/build.py builds it", RuntimeWarning,
@@ -342,6 +366,38 @@ class Cache:
                 raise ValueError("block_table must have one row per sequence")
         elif (self.k.shape[0], self.k.shape[1], self.k.shape[2], self.k.shape[4]) != (B, NL, H, D):
             raise ValueError("contiguous cache must be [B, NL, H, S_max, D]")
+
+
+class QuantCache:
+    """Decoder cache in 8 bits: codes k, v (float8_e4m3fn or int8), contiguous [B, NL, H, S_max, D] or
+    paged [NL, n_blocks, block_size, H, D] with block_table [B, max_blocks] int32, and a float32
+    scale per row, k_scale, v_scale [B, NL, H, S_max] or [NL, n_blocks, H, block_size].  A row stands
+    for its codes times its scale."""
+
+    def __init__(self, k, v, k_scale, v_scale, block_table=None):
+        torch = _torch()
+        _need(k, "cache.k", ndim=5)
+        if k.dtype not in (torch.float8_e4m3fn, torch.int8):
+            raise ValueError(f"unsupported code type {k.dtype} (float8_e4m3fn or int8)")
+        _need(v, "cache.v", dtype=k.dtype, ndim=5, device=k.device)
+        if v.shape != k.shape:
+            raise ValueError("cache.k and cache.v shapes differ")
+        if block_table is not None:
+            _need(block_table, "cache.block_table", torch.int32, 2, k.device)
+            shape = (k.shape[0], k.shape[1], k.shape[3], k.shape[2])
+        else:
+            shape = k.shape[:4]
+        for t, name in ((k_scale, "cache.k_scale"), (v_scale, "cache.v_scale")):
+            _need(t, name, torch.float32, 4, k.device)
+            _shape(t, name, shape)
+        self.k, self.v, self.k_scale, self.v_scale, self.block_table = k, v, k_scale, v_scale, block_table
+        self.paged = block_table is not None
+        self.device = k.device
+
+    def to_c(self) -> CQuantCache:
+        torch = _torch()
+        return CQuantCache(Cache.to_c(self), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                           PRCR_E4M3 if self.k.dtype == torch.float8_e4m3fn else PRCR_I8)
 
 
 def _selection(mem: Memory, sel_off, sel_idx):
@@ -857,3 +913,144 @@ def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, ke
         workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
     _check("prcr_evict", st)
     return new_cache_len, kept, new_weights
+
+
+def quant_append(rope: Rope, cache: QuantCache, layer: int, raw_k, raw_v, pos, n_tokens, cache_start,
+                 err=None, stream=None):
+    """Tokens of one layer appended to a cache in 8 bits (prcr_quant_append): raw_k, raw_v [B, S, H, D]
+    the layer's projections before rotary, pos [B, S, 3], the first n_tokens[b] rows of each sequence
+    to its slots from cache_start[b] on."""
+    done = (_NATIVE or _native()).quant_append(rope, cache, layer, raw_k, raw_v, pos, n_tokens, cache_start,
+                                               err, stream)
+    if done is not None:
+        return _done("prcr_quant_append", done)
+    layer = _int32(layer, "layer")
+    torch = _torch()
+    NL, H, D = _cache_dims(cache)
+    B = _batch(cache)
+    _need(raw_k, "raw_k", None, 4, cache.device)
+    _need(raw_v, "raw_v", raw_k.dtype, 4, cache.device)
+    dtype = _dtype_code(raw_k)
+    if raw_k.shape != raw_v.shape or raw_k.shape[0] != B or tuple(raw_k.shape[2:]) != (H, D):
+        raise ValueError("raw_k/raw_v must be [B, S_src, H, D]")
+    S = _int32(raw_k.shape[1], "raw_k size")
+    _need(pos, "pos", torch.int32, 3, cache.device)
+    _shape(pos, "pos", (B, S, 3))
+    _need(n_tokens, "n_tokens", torch.int32, 1, cache.device)
+    _shape(n_tokens, "n_tokens", (B,))
+    _need(cache_start, "cache_start", torch.int32, 1, cache.device)
+    _shape(cache_start, "cache_start", (B,))
+    _err(err, cache.device)
+    st = lib().prcr_quant_append(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL),
+                                 int(H), layer, _ptr(raw_k), _ptr(raw_v), S, _ptr(pos), _ptr(n_tokens),
+                                 _ptr(cache_start), _ptr(err), _stream(stream, cache.device))
+    _check("prcr_quant_append", st)
+
+
+def quant_rebind_inject(rope: Rope, mem: Memory, sel_off, sel_idx, new_pos, cache: QuantCache, cache_len,
+                        new_cache_len=None, slot_mapping=None, err=None, stream=None):
+    """rebind_inject into a cache in 8 bits (prcr_quant_rebind_inject).  Returns (new_cache_len [B]
+    int32, slot_mapping [total_k] int64)."""
+    done = (_NATIVE or _native()).quant_rebind_inject(rope, mem, sel_off, sel_idx, new_pos, cache, cache_len,
+                                                      new_cache_len, slot_mapping, err, stream)
+    if done is not None:
+        return _done("prcr_quant_rebind_inject", done)
+    torch = _torch()
+    total_k = _selection(mem, sel_off, sel_idx)
+    B, _, NL, H, D = mem.k.shape
+    if cache.device != mem.device:
+        raise ValueError(f"cache is on {cache.device}, expected {mem.device}")
+    if (_batch(cache), *_cache_dims(cache)) != (B, NL, H, D):
+        raise ValueError("cache and memory shapes differ")
+    _need(new_pos, "new_pos", torch.float64, 2, mem.device)
+    _shape(new_pos, "new_pos", (total_k, 3))
+    _need(cache_len, "cache_len", torch.int32, 1, mem.device)
+    _shape(cache_len, "cache_len", (B,))
+    if new_cache_len is None:
+        new_cache_len = _new((B,), torch.int32, mem.device, stream)
+    if slot_mapping is None:
+        slot_mapping = _new((total_k,), torch.int64, mem.device, stream)
+    _need(new_cache_len, "new_cache_len", torch.int32, 1, mem.device)
+    _need(slot_mapping, "slot_mapping", torch.int64, 1, mem.device)
+    _shape(new_cache_len, "new_cache_len", (B,))
+    _shape(slot_mapping, "slot_mapping", (total_k,))
+    _err(err, mem.device)
+    st = lib().prcr_quant_rebind_inject(
+        ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(new_pos),
+        ctypes.byref(cache.to_c()), _ptr(cache_len), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
+        _stream(stream, mem.device))
+    _check("prcr_quant_rebind_inject", st)
+    return new_cache_len, slot_mapping
+
+
+def quant_read(cache: QuantCache, layer: int, cache_len, dtype, k=None, v=None, err=None, stream=None):
+    """One layer of a cache in 8 bits read back into rows of dtype, float32 or bfloat16
+    (prcr_quant_read).  Returns (k, v) [B, 1, H, S, D], a contiguous cache of one layer; S is the
+    capacity, or that of the tensors given, whose slots from cache_len[b] on are not written."""
+    torch = _torch()
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"unsupported element type {dtype} (float32 or bfloat16)")
+    done = (_NATIVE or _native()).quant_read(cache, layer, cache_len, dtype == torch.float32, k, v, err, stream)
+    if done is not None:
+        return _done("prcr_quant_read", done)
+    layer = _int32(layer, "layer")
+    NL, H, D = _cache_dims(cache)
+    B = _batch(cache)
+    _need(cache_len, "cache_len", torch.int32, 1, cache.device)
+    _shape(cache_len, "cache_len", (B,))
+    if k is not None:
+        _need(k, "k", dtype, 5, cache.device)
+    S = _capacity(cache) if k is None else _int32(k.shape[3], "k size")
+    shape = (B, 1, H, S, D)
+    k = _new(shape, dtype, cache.device, stream) if k is None else k
+    v = _new(shape, dtype, cache.device, stream) if v is None else v
+    _need(v, "v", dtype, 5, cache.device)
+    _shape(k, "k", shape)
+    _shape(v, "v", shape)
+    _err(err, cache.device)
+    st = lib().prcr_quant_read(ctypes.byref(cache.to_c()), _dtype_code(k), int(B), int(NL), int(H), int(D), layer,
+                               _ptr(cache_len), _ptr(k), _ptr(v), S, _ptr(err), _stream(stream, cache.device))
+    _check("prcr_quant_read", st)
+    return k, v
+
+
+def quant_decode_workspace_bytes(cache: QuantCache, n_q_heads: int) -> int:
+    """Bytes of workspace prcr_quant_decode_attention needs (prcr_quant_decode_workspace_size)."""
+    NL, H, D = _cache_dims(cache)
+    return _size_t("prcr_quant_decode_workspace_size", ctypes.byref(cache.to_c()), _batch(cache),
+                   _int32(n_q_heads, "n_q_heads"), int(H), int(D))
+
+
+def quant_decode_attention(rope: Rope, cache: QuantCache, layer: int, q, q_pos, cache_len, scale=None, out=None,
+                           workspace=None, err=None, stream=None):
+    """decode_attention over one layer of a cache in 8 bits (prcr_quant_decode_attention).
+    q [B, Hq, D] raw queries, float32 or bfloat16; returns out float32 [B, Hq, D]."""
+    done = (_NATIVE or _native()).quant_decode_attention(rope, cache, layer, q, q_pos, cache_len, scale, out,
+                                                         workspace, err, stream)
+    if done is not None:
+        return _done("prcr_quant_decode_attention", done)
+    layer = _int32(layer, "layer")
+    torch = _torch()
+    NL, H, D = _cache_dims(cache)
+    B = _batch(cache)
+    _need(q, "q", None, 3, cache.device)
+    dtype = _dtype_code(q)
+    Hq = q.shape[1]
+    _shape(q, "q", (B, Hq, D))
+    _need(q_pos, "q_pos", torch.int32, 1, cache.device)
+    _shape(q_pos, "q_pos", (B,))
+    _need(cache_len, "cache_len", torch.int32, 1, cache.device)
+    _shape(cache_len, "cache_len", (B,))
+    if out is None:
+        out = _new((B, Hq, D), torch.float32, cache.device, stream)
+    _need(out, "out", torch.float32, 3, cache.device)
+    _shape(out, "out", (B, Hq, D))
+    workspace = _workspace(workspace, quant_decode_workspace_bytes(cache, Hq), cache.device, stream)
+    _err(err, cache.device)
+    sc = float(D) ** -0.5 if scale is None else float(scale)
+    st = lib().prcr_quant_decode_attention(
+        ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL), int(H), layer, _ptr(q), int(Hq),
+        _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
+    _check("prcr_quant_decode_attention", st)
+    return out

@@ -36,13 +36,13 @@ namespace {
 
 struct Skip {};   // not the plain case: binding.py takes the call
 
-PyObject *g_rope, *g_memory, *g_cache;   // the classes, exactly these
+PyObject *g_rope, *g_memory, *g_cache, *g_quant_cache;   // the classes, exactly these
 PyObject *g_modes;                       // mode name -> number
 PyObject *g_raw_stream;                  // device index -> the current stream's handle
 
 #define PRCR_NAMES(X)                                                                     \
   X(k) X(v) X(coords) X(n_visual) X(v_slot) X(device) X(block_table) X(paged) X(head_dim) \
-  X(sections) X(interleaved) X(theta) X(cuda_stream)
+  X(sections) X(interleaved) X(theta) X(cuda_stream) X(k_scale) X(v_scale)
 #define PRCR_DECLARE(n) PyObject *s_##n;
 PRCR_NAMES(PRCR_DECLARE)
 #undef PRCR_DECLARE
@@ -277,6 +277,49 @@ struct Store {
   at::Tensor k, v, table;
   bool paged;
   prcr_cache c{};
+};
+
+// A QuantCache's tensors, held for the call, and its descriptor.
+struct QuantStore {
+  explicit QuantStore(PyObject *o)
+      : owner((only(o, g_quant_cache), o)), device(device_of(o)), k(tensor_attr(o, s_k)), v(tensor_attr(o, s_v)),
+        k_scale(tensor_attr(o, s_k_scale)), v_scale(tensor_attr(o, s_v_scale)), paged(bool_of(attr(o, s_paged).get())) {
+    if (k.dim() != 5) throw Skip();
+    c.cache.k = ptr<void>(k);
+    c.cache.v = ptr<void>(v);
+    c.k_scale = ptr<float>(k_scale);
+    c.v_scale = ptr<float>(v_scale);
+    if (k.scalar_type() == at::kFloat8_e4m3fn)
+      c.code = PRCR_E4M3;
+    else if (k.scalar_type() == at::kChar)
+      c.code = PRCR_I8;
+    else
+      throw Skip();
+    c.cache.paged = paged ? 1 : 0;
+    if (paged) {
+      table = tensor_attr(o, s_block_table);
+      if (table.dim() != 2) throw Skip();
+      c.cache.block_table = ptr<int32_t>(table);
+      c.cache.block_size = to_int32(k.size(2));
+      c.cache.max_blocks = to_int32(table.size(1));
+      c.cache.n_blocks = to_int32(k.size(1));
+    } else {
+      c.cache.s_max = to_int32(k.size(3));
+    }
+    batch = to_int32(paged ? table.size(0) : k.size(0));
+    n_layers = to_int32(k.size(paged ? 0 : 1));
+    n_kv_heads = to_int32(k.size(paged ? 3 : 2));
+    head_dim = to_int32(k.size(4));
+  }
+  int64_t capacity() const {
+    return paged ? static_cast<int64_t>(c.cache.max_blocks) * c.cache.block_size : int64_t{c.cache.s_max};
+  }
+  PyObject *owner;
+  at::Device device;
+  at::Tensor k, v, k_scale, v_scale, table;
+  bool paged;
+  int32_t batch, n_layers, n_kv_heads, head_dim;
+  prcr_quant_cache c{};
 };
 
 // The selection both calls of a revisit take.
@@ -701,14 +744,134 @@ PyObject *evict(Args a) {
   return done(st, &failed) ? tuple_of(new_len.t, kept.t, new_weights.t) : failed;
 }
 
-// (Rope, Memory, Cache, MODES), once.
+// (rope, cache, layer, raw_k, raw_v, pos, n_tokens, cache_start, err, stream)
+PyObject *quant_append(Args a) {
+  const prcr_rope rope = rope_of(a[0]);
+  const QuantStore cache(a[1]);
+  const int32_t layer = int32_of(a[2]);
+  const at::Tensor raw_k = tensor(a[3]), raw_v = tensor(a[4]), pos = tensor(a[5]), n_tokens = tensor(a[6]),
+                   start = tensor(a[7]);
+  if (raw_k.dim() != 4) throw Skip();
+  const prcr_dtype dtype = dtype_of(raw_k);
+  const int64_t B = cache.batch, S = raw_k.size(1);
+  const at::DimVector shape{B, S, cache.n_kv_heads, cache.head_dim};
+  need(raw_k, raw_k.scalar_type(), cache.device, shape);
+  need(raw_v, raw_k.scalar_type(), cache.device, shape);
+  need(pos, at::kInt, cache.device, {B, S, 3});
+  need(n_tokens, at::kInt, cache.device, {B});
+  need(start, at::kInt, cache.device, {B});
+  const at::Tensor err = err_of(a[8], cache.device);
+  const Launch on(a[9], cache.device);
+  const int32_t s_src = to_int32(S);
+  prcr_status st;
+  {
+    Unlocked u;
+    st = prcr_quant_append(&rope, &cache.c, dtype, cache.batch, cache.n_layers, cache.n_kv_heads, layer, ptr<void>(raw_k),
+                           ptr<void>(raw_v), s_src, ptr<int32_t>(pos), ptr<int32_t>(n_tokens), ptr<int32_t>(start),
+                           ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? Py_NewRef(Py_True) : failed;
+}
+
+// (rope, mem, sel_off, sel_idx, new_pos, cache, cache_len, new_cache_len, slot_mapping, err, stream)
+PyObject *quant_rebind_inject(Args a) {
+  const prcr_rope rope = rope_of(a[0]);
+  const Mem m(a[1]);
+  const Selection sel(m, a[2], a[3]);
+  const at::Tensor new_pos = tensor(a[4]), cache_len = tensor(a[6]);
+  const QuantStore cache(a[5]);
+  if (cache.device != m.device || cache.batch != m.c.batch || cache.n_layers != m.c.n_layers ||
+      cache.n_kv_heads != m.c.n_kv_heads || cache.head_dim != m.c.head_dim)
+    throw Skip();
+  need(new_pos, at::kDouble, m.device, {sel.k, 3});
+  need(cache_len, at::kInt, m.device, {m.c.batch});
+  Out new_len(a[7], at::kInt, m.device, {m.c.batch}), slots(a[8], at::kLong, m.device, {sel.k});
+  const at::Tensor err = err_of(a[9], m.device);
+  const Launch on(a[10], m.device);
+  prcr_status st;
+  {
+    Unlocked u;
+    new_len.make(on);
+    slots.make(on);
+    st = prcr_quant_rebind_inject(&rope, &m.c, ptr<int32_t>(sel.off), ptr<int32_t>(sel.idx), sel.k, ptr<double>(new_pos),
+                                  &cache.c, ptr<int32_t>(cache_len), ptr<int32_t>(new_len.t), ptr<int64_t>(slots.t),
+                                  ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? tuple_of(new_len.t, slots.t) : failed;
+}
+
+// (cache, layer, cache_len, dtype, k, v, err, stream); dtype: float32 or not (bfloat16)
+PyObject *quant_read(Args a) {
+  const QuantStore cache(a[0]);
+  const int32_t layer = int32_of(a[1]);
+  const at::Tensor cache_len = tensor(a[2]);
+  const at::ScalarType type = bool_of(a[3]) ? at::kFloat : at::kBFloat16;
+  need(cache_len, at::kInt, cache.device, {cache.batch});
+  const at::Tensor given = tensor_or_none(a[4]);
+  if (given.defined() && given.dim() != 5) throw Skip();
+  const int64_t S = given.defined() ? given.size(3) : cache.capacity();
+  const at::DimVector shape{cache.batch, 1, cache.n_kv_heads, S, cache.head_dim};
+  Out k(a[4], type, cache.device, shape), v(a[5], type, cache.device, shape);
+  const at::Tensor err = err_of(a[6], cache.device);
+  const Launch on(a[7], cache.device);
+  const int32_t s_out = to_int32(S);
+  prcr_status st;
+  {
+    Unlocked u;
+    k.make(on);
+    v.make(on);
+    st = prcr_quant_read(&cache.c, dtype_of(k.t), cache.batch, cache.n_layers, cache.n_kv_heads, cache.head_dim, layer,
+                         ptr<int32_t>(cache_len), ptr<void>(k.t), ptr<void>(v.t), s_out, ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? tuple_of(k.t, v.t) : failed;
+}
+
+// (rope, cache, layer, q, q_pos, cache_len, scale, out, workspace, err, stream)
+PyObject *quant_decode_attention(Args a) {
+  const prcr_rope rope = rope_of(a[0]);
+  const QuantStore cache(a[1]);
+  const int32_t layer = int32_of(a[2]);
+  const at::Tensor q = tensor(a[3]), q_pos = tensor(a[4]), cache_len = tensor(a[5]);
+  if (q.dim() != 3) throw Skip();
+  const prcr_dtype dtype = dtype_of(q);
+  const int64_t B = cache.batch, Hq = q.size(1), D = cache.head_dim;
+  need(q, q.scalar_type(), cache.device, {B, Hq, D});
+  need(q_pos, at::kInt, cache.device, {B});
+  need(cache_len, at::kInt, cache.device, {B});
+  const double scale = a[6] == Py_None ? std::pow(static_cast<double>(D), -0.5) : double_of(a[6]);
+  Out out(a[7], at::kFloat, cache.device, {B, Hq, D});
+  const int32_t hq = to_int32(Hq);
+  size_t bytes = 0;
+  if (prcr_quant_decode_workspace_size(&cache.c, cache.batch, hq, cache.n_kv_heads, cache.head_dim, &bytes) != PRCR_OK)
+    throw Skip();
+  Workspace ws(a[8], cache.device, bytes);
+  const at::Tensor err = err_of(a[9], cache.device);
+  const Launch on(a[10], cache.device);
+  prcr_status st;
+  {
+    Unlocked u;
+    out.make(on);
+    ws.make(on);
+    st = prcr_quant_decode_attention(&rope, &cache.c, dtype, cache.batch, cache.n_layers, cache.n_kv_heads, layer,
+                                     ptr<void>(q), hq, ptr<int32_t>(q_pos), ptr<int32_t>(cache_len),
+                                     static_cast<float>(scale), ptr<float>(out.t), ptr<void>(ws.t), ws.t.nbytes(),
+                                     ptr<int32_t>(err), on.handle());
+  }
+  PyObject *failed;
+  return done(st, &failed) ? wrap(out.t) : failed;
+}
+
+// (Rope, Memory, Cache, MODES, QuantCache), once.
 PyObject *setup(PyObject *, Args a, Py_ssize_t n) {
-  if (n != 4 || !PyDict_CheckExact(a[3])) {
-    PyErr_SetString(PyExc_TypeError, "setup(Rope, Memory, Cache, MODES)");
+  if (n != 5 || !PyDict_CheckExact(a[3])) {
+    PyErr_SetString(PyExc_TypeError, "setup(Rope, Memory, Cache, MODES, QuantCache)");
     return nullptr;
   }
-  PyObject **to[] = {&g_rope, &g_memory, &g_cache, &g_modes};
-  for (int i = 0; i < 4; ++i) Py_XSETREF(*to[i], Py_NewRef(a[i]));
+  PyObject **to[] = {&g_rope, &g_memory, &g_cache, &g_modes, &g_quant_cache};
+  for (int i = 0; i < 5; ++i) Py_XSETREF(*to[i], Py_NewRef(a[i]));
   Py_RETURN_NONE;
 }
 
@@ -726,6 +889,10 @@ PyMethodDef methods[] = {
     PRCR_ENTRY(chunk_attention, 14, chunk_attention),
     PRCR_ENTRY(key_weights, 16, key_weights),
     PRCR_ENTRY(evict, 13, evict),
+    PRCR_ENTRY(quant_append, 10, quant_append),
+    PRCR_ENTRY(quant_rebind_inject, 11, quant_rebind_inject),
+    PRCR_ENTRY(quant_read, 8, quant_read),
+    PRCR_ENTRY(quant_decode_attention, 11, quant_decode_attention),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_prcr_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
