@@ -41,9 +41,9 @@ struct QuantWriteParams {
   int32_t batch, s_src, max_visual, layer;
   int32_t n_tok;                  // tokens: batch * s_src, or total_k
   int32_t rows;                   // (layer, head) rows of a token: n_kv_heads, or n_layers * n_kv_heads
-  int32_t rows_per_wave;          // (launcher)
+  int32_t rows_per_group;         // of those, a workgroup's (launcher)
   Divisor by_seq, by_heads;
-  int8_t axis[kMaxPairs];
+  uint64_t on_h, on_w;            // pairs that turn by the h and by the w position (the others: t)
   double inv_freq[kMaxPairs];
 };
 
@@ -69,29 +69,40 @@ hipError_t launch_quant_decode(const QuantDecodeParams &p, prcr_code code, int h
 #ifdef __HIPCC__
 namespace {
 
-// Bases of a sequence's slot; flag: what is wrong with it (then they are not to be used).
+// Where a sequence's slot lies: in two steps, so that a paged cache's table entry, read from a
+// clamped place (always in the table), can be on its way with other loads.
+struct SlotEntry {
+  int64_t slot;
+  int64_t lb;                     // paged: the logical block, -1 outside the table
+  int32_t blk;                    // and its entry
+};
+__device__ __forceinline__ SlotEntry entry_of_slot(const QuantStore &s, int b, int64_t slot) {
+  SlotEntry e{slot, 0, 0};
+  if (s.paged) {
+    const bool in = slot >= 0 && slot < static_cast<int64_t>(s.max_blocks) * s.block_size;   // (at most 2^30)
+    e.lb = in ? static_cast<int64_t>(s.by_block.divide(static_cast<uint32_t>(slot))) : -1;
+    e.blk = s.block_table[static_cast<int64_t>(b) * s.max_blocks + (in ? e.lb : 0)];
+  }
+  return e;
+}
+// Bases of the slot; flag: what is wrong with it (then they are not to be used).
 struct Place {
   int64_t row, scale;
   int64_t id;                     // contiguous b s_max + slot, paged block block_size + offset
   int flag;
 };
-__device__ __forceinline__ Place place_of(const QuantStore &s, int b, int64_t slot) {
+__device__ __forceinline__ Place place_of(const QuantStore &s, int b, const SlotEntry &e) {
   Place at{0, 0, -1, 0};
   if (s.paged) {
-    const bool in = slot >= 0 && slot < static_cast<int64_t>(s.max_blocks) * s.block_size;
-    // (the capacity is at most 2^30)
-    const uint32_t lb = in ? s.by_block.divide(static_cast<uint32_t>(slot)) : 0u;
-    const int64_t off = in ? slot - static_cast<int64_t>(lb) * s.block_size : 0;
-    const int32_t blk = s.block_table[static_cast<int64_t>(b) * s.max_blocks + lb];
-    const bool ok = blk >= 0 && blk < s.n_blocks;
-    at.flag = !in ? PRCR_DERR_CAPACITY : (ok ? 0 : PRCR_DERR_BLOCK);
-    at.id = static_cast<int64_t>(blk) * s.block_size + off;
+    const int64_t off = e.slot - e.lb * s.block_size;
+    at.flag = e.lb < 0 ? PRCR_DERR_CAPACITY : (e.blk >= 0 && e.blk < s.n_blocks ? 0 : PRCR_DERR_BLOCK);
+    at.id = static_cast<int64_t>(e.blk) * s.block_size + off;
     at.row = at.id * s.n_kv_heads;
-    at.scale = static_cast<int64_t>(blk) * s.n_kv_heads * s.block_size + off;
+    at.scale = static_cast<int64_t>(e.blk) * s.n_kv_heads * s.block_size + off;
   } else {
-    at.flag = slot >= 0 && slot < s.s_max ? 0 : PRCR_DERR_CAPACITY;
-    at.id = static_cast<int64_t>(b) * s.s_max + slot;
-    at.row = at.scale = static_cast<int64_t>(b) * s.n_layers * s.n_kv_heads * s.s_max + slot;
+    at.flag = e.slot >= 0 && e.slot < s.s_max ? 0 : PRCR_DERR_CAPACITY;
+    at.id = static_cast<int64_t>(b) * s.s_max + e.slot;
+    at.row = at.scale = static_cast<int64_t>(b) * s.n_layers * s.n_kv_heads * s.s_max + e.slot;
   }
   return at;
 }

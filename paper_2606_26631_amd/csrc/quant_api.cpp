@@ -125,7 +125,9 @@ QuantStore store_of(const prcr_quant_cache &cache, int32_t n_layers, int32_t n_k
 
 void set_rope(const prcr_rope &rope, AxisMapId map, QuantWriteParams *p) {
   for (int i = 0; i < rope.head_dim / 2; ++i) {
-    p->axis[i] = static_cast<int8_t>(axis_of_pair(map, i));
+    const int axis = axis_of_pair(map, i);
+    p->on_h |= static_cast<uint64_t>(axis == 1) << i;
+    p->on_w |= static_cast<uint64_t>(axis == 2) << i;
     p->inv_freq[i] = std::pow(rope.theta, -(2.0 * i) / rope.head_dim);
   }
 }

@@ -166,16 +166,20 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
     }
     return t;
   };
-  const uint32_t row_step = kPaged ? static_cast<uint32_t>(p.n_kv_heads) * D : D;
-  // Byte offset of key t (t / 16 == half).
-  auto key_offset = [&](const TileRows &tr, int t, int half) -> int64_t {
-    if constexpr (!kPaged)
-      return tr.base[0] * D + static_cast<uint32_t>(min(t, tr.last[0])) * row_step;
-    else if constexpr (kHalfBlocks)
-      return tr.base[half] * D + static_cast<uint32_t>(min(t - 16 * half, tr.last[half])) * row_step;
-    else
-      return (row_layer + static_cast<int64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(tr.slot), lane_of(t))))) *
-                 row_step + static_cast<int64_t>(kvh) * D;
+  const uint32_t row_step = kPaged ? static_cast<uint32_t>(p.n_kv_heads) * D : D;   // (below 2^23)
+  // Where byte `at` of key t's row is in an array (t / 16 == half): a base that all lanes share, and
+  // 32 bits of a lane's own.
+  auto in_row = [&](const char *cache, const TileRows &tr, int t, int half, uint32_t at) -> const char * {
+    if constexpr (!kPaged) {
+      const char *const base = cache + tr.base[0] * D;
+      return base + (static_cast<uint32_t>(min(t, tr.last[0])) * D + at);
+    } else if constexpr (kHalfBlocks) {
+      const char *const base = cache + tr.base[half] * D;
+      return base + (__umul24(static_cast<uint32_t>(min(t - 16 * half, tr.last[half])), row_step) + at);
+    } else {
+      const uint32_t slot = static_cast<uint32_t>(__shfl(static_cast<int>(tr.slot), lane_of(t)));
+      return cache + (row_layer + static_cast<int64_t>(slot)) * row_step + (static_cast<uint32_t>(kvh) * D + at);
+    }
   };
   // Key rows, whole lines once, past the caches: load 0 of 128 features reads the rows of columns
   // 0..7, load 1 those of columns 8..15, a half of a row in the lanes of its own column and the
@@ -187,11 +191,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
       if constexpr (kKL == 2) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          kd[st][u] = load_nt(cache_k + key_offset(tr, ka + 4 * st + 16 * u, u) + (n16 / 8) * 64 + kj * 16);
+          kd[st][u] = load_nt(in_row(cache_k, tr, ka + 4 * st + 16 * u, u, (n16 / 8) * 64 + kj * 16));
       } else {
         const int t = 8 * (n16 / 4) + 4 * st + n16 % 4;
-        const int64_t lo = key_offset(tr, t, 0), hi = key_offset(tr, t, 1);   // (one of them is the key's)
-        kd[st][0] = load_nt(cache_k + (n16 < 8 ? lo : hi) + kj * 16);
+        const char *const lo = in_row(cache_k, tr, t, 0, kj * 16), *const hi = in_row(cache_k, tr, t, 1, kj * 16);
+        kd[st][0] = load_nt(n16 < 8 ? lo : hi);   // (one of them is the key's)
       }
     }
   };
@@ -199,8 +203,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   auto load_v = [&](const TileRows &tr, vrow (&vd)[kVL]) {
 #pragma unroll
     for (int u = 0; u < kVL; ++u) {
-      const int64_t o = key_offset(tr, 4 * u + kj, u / 4);
-      vd[u] = __builtin_nontemporal_load(reinterpret_cast<const vrow *>(cache_v + o + n16 * kDL));
+      vd[u] = __builtin_nontemporal_load(reinterpret_cast<const vrow *>(in_row(cache_v, tr, 4 * u + kj, u / 4, n16 * kDL)));
     }
   };
 
@@ -302,6 +305,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
     load_k(tr, kr);
 
     const bool live0 = (live >> n16) & 1u, live1 = (live >> (16 + n16)) & 1u;
+    vs[0] = live0 ? vs[0] : 0.f;
+    vs[1] = live1 ? vs[1] : 0.f;
     float sc[kA][2];
     bool rise = false;
 #pragma unroll
@@ -309,7 +314,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
         const float s = ((sa[a][st][0] + sa[a][st][1]) + sa[a][st][2]) * ks[st];
-        sc[a][st] = (st == 0 ? live0 : live1) ? s : -FLT_MAX;
+        sc[a][st] = (st == 0 ? live0 : live1) ? s : -INFINITY;
         rise = rise || sc[a][st] > mrun[a];
       }
     }
@@ -343,12 +348,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
       uint32_t part[3][2];
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const bool on = st == 0 ? live0 : live1;
-        const float w = on ? exp2_fast(sc[a][st] - mrun[a]) : 0.f;
+        const float w = exp2_fast(sc[a][st] - mrun[a]);   // (0 where the key has no weight)
         lsum[a] += w;
-        const float wv = on ? w * vs[st] : 0.f;
 #pragma unroll
-        for (int q = 0; q < 3; ++q) part[q][st] = split_part(wv, q);
+        for (int q = 0; q < 3; ++q) part[q][st] = split_part(w * vs[st], q);
       }
 #pragma unroll
       for (int q = 0; q < 3; ++q) {

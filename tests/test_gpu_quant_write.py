@@ -93,7 +93,7 @@ def test_many_tokens(dtype, kind):
 
 def edge_rows(dtype, D):
     """Rows where the format is at its edges: zeros, the smallest numbers, infinities, NaN, rows of one large
-    element, halves of a code's step, and every bf16 magnitude."""
+    element, halves of a code's step, every bf16 magnitude; and ordinary ones in number."""
     rng = np.random.default_rng(5)
     rows = [np.zeros(D), np.full(D, -0.0), np.full(D, 2.0 ** -149), np.full(D, 1e-38), np.full(D, 3.3e38)]
     for value in (np.inf, -np.inf, np.nan):
@@ -116,6 +116,7 @@ def edge_rows(dtype, D):
         rows.append(r)
     bits = np.arange(0x7F80, dtype=np.uint32)  # every finite bf16 magnitude, D to a row, largest of each row its last
     rows += list((bits[:len(bits) // D * D] << 16).view(np.float32).reshape(-1, D).astype(np.float64))
+    rows += list(rng.standard_normal((4000, D)) * np.exp(rng.standard_normal((4000, 1))))
     with np.errstate(over="ignore"):
         x = torch.from_numpy(np.array(rows, np.float32)).to(TYPES[dtype])
     return x
