@@ -319,7 +319,7 @@ __global__ __launch_bounds__(kWaves * kWave, GT == 8 && D == 128 ? 2 : 3) void d
   const int lane = threadIdx.x & (kWave - 1);
   const double inv = p.inv_freq[threadIdx.x % P];
   int len_in;
-  const int b = sequence_of_row<kWaves>(p, lane, row_of(p, split), &len_in);
+  const int b = sequence_of_row<kWaves>(p, lane, row_of(p, split, static_cast<int>(blockIdx.y)), &len_in);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n16 = lane % 16;                 // product column; operand row
   const int kj = lane / 16;                  // k group of the operands; head of the lane's scores
@@ -894,21 +894,7 @@ void plan_splits(DecodeParams *p, prcr_dtype dtype, bool paged) {
   p->fill = p->n_split;
   p->min_keys = 0;
   if (dtype == PRCR_F32) return;
-  auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  // The first splits for lo to hi workgroups that come within 3 % of whole rounds over the
-  // chip, or else the nearest (a search of at most some tens of steps, on every call).
-  auto rounds = [&](int64_t lo, int64_t hi) {
-    int64_t best = ceil_div(lo, pairs);
-    double share = 0;
-    for (int64_t n = best; n <= std::min(ceil_div(hi, pairs), room) && share < 0.97; ++n) {
-      const double s = static_cast<double>(pairs * n) / static_cast<double>(ceil_div(pairs * n, kUnits) * kUnits);
-      if (s > share + 1e-9) {
-        share = s;
-        best = n;
-      }
-    }
-    return std::min(best, room);
-  };
+  auto rounds = [&](int64_t lo, int64_t hi) { return splits_in_rounds(pairs, lo, hi, room, 0.97); };
   const int64_t fill = pairs >= 3 * kUnits / 4 ? 1 : rounds(3 * kUnits / 4, 2 * kUnits);
   const int64_t most = capacity / kMinKeys;
   const int64_t more = most >= std::min(ceil_div(2 * kUnits, pairs), room) ? rounds(2 * kUnits, 4 * kUnits) : fill;

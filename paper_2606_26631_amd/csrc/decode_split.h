@@ -3,6 +3,7 @@
 // bf16 operands of float32 numbers.
 #pragma once
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstdint>
@@ -18,6 +19,24 @@ hipError_t launch_decode_merge(const DecodeParams &p, int head_dim, bool paged, 
 namespace {
 
 constexpr int kUnits = 256;  // compute units of the chip
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The first splits of `pairs` (sequence, KV head) pairs for lo to hi workgroups that fill whole rounds over
+// the chip to the share `enough`, or else the nearest; at most `room` (a search of at most some tens
+// of steps, on every call).
+inline int64_t splits_in_rounds(int64_t pairs, int64_t lo, int64_t hi, int64_t room, double enough) {
+  int64_t best = ceil_div(lo, pairs);
+  double share = 0;
+  for (int64_t n = best; n <= std::min(ceil_div(hi, pairs), room) && share < enough; ++n) {
+    const double s = static_cast<double>(pairs * n) / static_cast<double>(ceil_div(pairs * n, kUnits) * kUnits);
+    if (s > share + 1e-9) {
+      share = s;
+      best = n;
+    }
+  }
+  return std::min(best, room);
+}
 
 // Scores are kept in base-2 units (the query carries log2(e)), so every
 // softmax weight is one hardware exp2.
@@ -108,8 +127,7 @@ __device__ __forceinline__ int sequence_of_row(const DecodeParams &p, int lane, 
 // in two splits took 230.0 us with the splits innermost, 243.2 with the rows in the same
 // order in both splits and 215.7 this way.  The float32 kernel has three rounds, and is
 // faster with the splits innermost (238.8 against 257.3 us, 32 such sequences, 4 heads).
-__device__ __forceinline__ int row_of(const DecodeParams &p, int split) {
-  const int y = static_cast<int>(blockIdx.y);
+__device__ __forceinline__ int row_of(const DecodeParams &p, int split, int y) {
   const uint32_t before = static_cast<uint32_t>(split) * gridDim.x * gridDim.y;   // workgroups of earlier splits
   return before / kUnits & 1 ? p.batch - 1 - y : y;
 }

@@ -10,6 +10,7 @@
 // sums float32.  The key's scale multiplies the score, and the value's the weight before it is
 // split: neither costs an operation per element.
 #include <algorithm>
+#include <type_traits>
 
 #include "attend.h"
 #include "decode_split.h"
@@ -56,11 +57,25 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   __shared__ float s_l[kWaves][GT];
   __shared__ __align__(16) float s_o[kWaves][16][D];
 
-  const int split = blockIdx.z, kvh = blockIdx.x;
+  // Paged rows of 64 codes: two heads of a slot share a cache line.  Their workgroups are 8 apart, on one
+  // chip die (workgroups are dealt to the 8 dies in turn), and read through its cache, so that the line comes
+  // from memory once: 64 sequences of 2,000-4,000 keys, 8 heads of 64, 74 us, and 56 so (61 with reads past
+  // the caches, 71 without the order).
+  constexpr bool kHalfLines = D == 64 && kPaged;
+  int kvh = blockIdx.x, row_y = blockIdx.y;
+  if constexpr (kHalfLines) {
+    const uint32_t id = blockIdx.x + gridDim.x * blockIdx.y, heads = gridDim.x;
+    if (heads % 2 == 0 && id < heads * gridDim.y / 16 * 16) {
+      const uint32_t pair = id / 16 * 8 + id % 8;
+      kvh = static_cast<int>(2 * (pair % (heads / 2)) + id / 8 % 2);
+      row_y = static_cast<int>(pair / (heads / 2));
+    }
+  }
+  const int split = blockIdx.z;
   const int lane = threadIdx.x & (kWave - 1);
   const double inv = p.inv_freq[threadIdx.x % P];
   int len_in;
-  const int b = sequence_of_row<kWaves>(p, lane, row_of(p, split), &len_in);
+  const int b = sequence_of_row<kWaves>(p, lane, row_of(p, split, row_y), &len_in);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n16 = lane % 16;                 // product column; operand row
   const int kj = lane / 16;                  // k group of the operands; head of the lane's scores
@@ -195,7 +210,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
       } else {
         const int t = 8 * (n16 / 4) + 4 * st + n16 % 4;
         const char *const lo = in_row(cache_k, tr, t, 0, kj * 16), *const hi = in_row(cache_k, tr, t, 1, kj * 16);
-        kd[st][0] = load_nt(n16 < 8 ? lo : hi);   // (one of them is the key's)
+        const char *const at = n16 < 8 ? lo : hi;
+        kd[st][0] = kHalfLines ? *reinterpret_cast<const u32x4 *>(at) : load_nt(at);   // (one of them is the key's)
       }
     }
   };
@@ -203,7 +219,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   auto load_v = [&](const TileRows &tr, vrow (&vd)[kVL]) {
 #pragma unroll
     for (int u = 0; u < kVL; ++u) {
-      vd[u] = __builtin_nontemporal_load(reinterpret_cast<const vrow *>(in_row(cache_v, tr, 4 * u + kj, u / 4, n16 * kDL)));
+      const vrow *const at = reinterpret_cast<const vrow *>(in_row(cache_v, tr, 4 * u + kj, u / 4, n16 * kDL));
+      vd[u] = kHalfLines ? *at : __builtin_nontemporal_load(at);
     }
   };
 
@@ -437,9 +454,44 @@ void launch_one(const QuantDecodeParams &p, bool paged, hipStream_t stream) {
 template <int D, int GT>
 void launch_code(const QuantDecodeParams &p, prcr_code code, bool paged, hipStream_t stream) {
   if (code == PRCR_E4M3)
-    launch_one<D, GT, true, 4>(p, paged, stream);
+    p.waves == 8 ? launch_one<D, GT, true, 8>(p, paged, stream) : launch_one<D, GT, true, 4>(p, paged, stream);
   else
-    launch_one<D, GT, false, 4>(p, paged, stream);
+    p.waves == 8 ? launch_one<D, GT, false, 8>(p, paged, stream) : launch_one<D, GT, false, 4>(p, paged, stream);
+}
+
+// How a call is split, within the room for decode_splits' partials (p->n_split on entry).  As decode.hip's
+// plan, only the sequence's length and the call's shape enter, and half the bytes a key move its borders:
+//   - a cache of at most 1,024 slots (head_dim 64: 2,048) is one chunk a sequence: 8 sequences of 400-800
+//     keys, 8 KV heads, take 9.7 us so, in chunks and a merge 10.4; one of 1,152 keys 10.2 and 9.9;
+//   - else one workgroup per compute unit, and two to four, of 1,024 keys and more, where there are several
+//     sequences, which may differ in length: 64 of 2,912-6,512 keys, 4 KV heads, 62 us in two chunks and 69 in one
+//     (32 of 2,756-4,256, 8 KV heads, 41 and 40; one of 120,001 42 in 32 and 43 in 64; 64 of
+//     1,000-2,000, 4 KV heads, 25 in two and 23 in one).
+// A sequence that is one chunk is read by eight waves where they are few, or have half the bytes a key
+// (one of 600 keys: 7.7 us, with four waves 8.1; 32 of 1,000-2,000, 8 heads of 64: 11.7 and 14.3; but 64
+// of 1,000-2,000, 4 heads of 128, 24.1 and 23.0).  More than about 42 GB/s a compute unit does not read.
+void plan(QuantDecodeParams *p, int head_dim, bool paged) {
+  const int64_t room = p->n_split, pairs = static_cast<int64_t>(p->batch) * p->n_kv_heads;
+  const int64_t capacity = paged ? static_cast<int64_t>(p->max_blocks) * p->block_size : p->s_max;
+  constexpr int kMinKeys = 1024;
+  int64_t fill = 1, n = 1;
+  if (capacity > (head_dim == 64 ? 2048 : 1024)) {
+    fill = pairs >= 3 * kUnits / 4 ? 1 : splits_in_rounds(pairs, 3 * kUnits / 4, 2 * kUnits, room, 0.9);
+    n = fill;
+    if (p->batch > 1 && capacity / kMinKeys >= std::min(ceil_div(2 * kUnits, pairs), room)) {
+      const int64_t more = splits_in_rounds(pairs, 2 * kUnits, 4 * kUnits, room, 0.9);
+      if (capacity / kMinKeys >= more) n = std::max(fill, more);
+    }
+  }
+  p->n_split = static_cast<int32_t>(n);
+  p->fill = static_cast<int32_t>(fill);
+  p->min_keys = kMinKeys / 2;                // (of a chunk of a shorter sequence)
+  p->waves = n == 1 && (head_dim == 64 || pairs <= kUnits / 2) ? 8 : 4;
+  p->round = p->waves * kTile;
+  auto inverse = [](int64_t m) { return m > 1 ? static_cast<uint32_t>(((int64_t{1} << 32) + m - 1) / m) : 0u; };
+  p->split_inverse = inverse(n);
+  p->fill_inverse = inverse(fill);
+  p->direct = n == 1;
 }
 
 }  // namespace
@@ -447,14 +499,7 @@ void launch_code(const QuantDecodeParams &p, prcr_code code, bool paged, hipStre
 hipError_t launch_quant_decode(const QuantDecodeParams &in, prcr_code code, int head_dim, bool paged, hipStream_t stream) {
   QuantDecodeParams p = in;
   p.group = p.n_q_heads / p.n_kv_heads;
-  p.waves = 4;
-  p.fill = p.n_split;
-  p.min_keys = 0;
-  p.round = p.waves * kTile;
-  auto inverse = [](int64_t n) { return n > 1 ? static_cast<uint32_t>(((int64_t{1} << 32) + n - 1) / n) : 0u; };
-  p.split_inverse = inverse(p.n_split);
-  p.fill_inverse = inverse(p.fill);
-  p.direct = p.n_split == 1;
+  plan(&p, head_dim, paged);
   if (head_dim == 64)
     p.group <= 4 ? launch_code<64, 4>(p, code, paged, stream) : launch_code<64, 8>(p, code, paged, stream);
   else
