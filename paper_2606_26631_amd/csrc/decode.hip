@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kWaves * kWave) void decode_partial_kernel(const De
     }
   }
   __syncthreads();
-  finish_split<kWaves, D, GT, 1, 1>(p, b, kvh, G, split, s_m, s_l, s_o);
+  finish_split<kWaves, D, GT, 1, 1>(p, b, kvh, G, split, static_cast<int>(threadIdx.x), s_m, s_l, s_o);
 }
 
 // ---------------------------------------------------------------------------
@@ -658,7 +658,7 @@ __global__ __launch_bounds__(kWaves * kWave, GT == 8 && D == 128 ? 2 : 3) void d
           f32x4{acc[4 * c][r], acc[4 * c + 1][r], acc[4 * c + 2][r], acc[4 * c + 3][r]};
   }
   __syncthreads();
-  finish_split<kWaves, D, GT, GT == 4 ? 3 : 2, GT>(p, b, kvh, G, split, s_m, s_l, s_o);
+  finish_split<kWaves, D, GT, GT == 4 ? 3 : 2, GT>(p, b, kvh, G, split, static_cast<int>(threadIdx.x), s_m, s_l, s_o);
 }
 
 // Over the wave's four rows of 16 lanes (the same value in every lane): register lane

@@ -156,19 +156,19 @@ __device__ __forceinline__ int clamp_len(const DecodeParams &p, bool paged, int 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // at any float
 
-// Ends a workgroup's chunk: merges its waves' running maxima, sums of weights and weighted
+// Ends a chunk of kWaves waves (`thread` among them): merges the waves' running maxima, sums of weights and weighted
 // values (a head's value is the sum of kParts rows, kStep rows apart) and writes them to the
 // workspace for decode_combine_kernel, or, where every sequence is one chunk (p.direct), to
 // the output at once.  Four features of one head per thread, every LDS read issued before
 // the first use; a feature at a time this took 0.6 us of the 4 us that a short chunk takes.
 template <int kWaves, int D, int GT, int kParts, int kStep, int kRows>
-__device__ __forceinline__ void finish_split(const DecodeParams &p, int b, int kvh, int G, int split,
+__device__ __forceinline__ void finish_split(const DecodeParams &p, int b, int kvh, int G, int split, int thread,
                                              const float (&s_m)[kWaves][GT], const float (&s_l)[kWaves][GT],
                                              const float (&s_o)[kWaves][kRows][D]) {
   const int64_t head0 = static_cast<int64_t>(b) * p.n_q_heads + kvh * G;
 #pragma unroll
   for (int u = 0; u < (GT * D / 4 + kWaves * kWave - 1) / (kWaves * kWave); ++u) {
-    const int idx = u * kWaves * kWave + threadIdx.x;
+    const int idx = u * kWaves * kWave + thread;
     const int g = idx / (D / 4), d = idx % (D / 4) * 4;
     if (g >= G) break;
     float m[kWaves], l[kWaves];

@@ -59,6 +59,7 @@ struct QuantReadParams {
 struct QuantDecodeParams : DecodeParams {
   const float *k_scale, *v_scale;
   int32_t q_f32;                  // the queries' type
+  int32_t heads;                  // KV heads of a workgroup (launcher)
 };
 
 hipError_t launch_quant_append(const QuantWriteParams &p, prcr_dtype dtype, int head_dim, hipStream_t stream);

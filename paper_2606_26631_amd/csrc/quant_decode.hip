@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t codes2(uint32_t w) {
 // GT: query heads per KV head there is room for (4 or 8; smaller groups repeat their first head).
 // kHalfBlocks (paged only): block_size is a multiple of 16, so that each half of a tile (tiles
 // start at multiples of 32) lies in one block; other block sizes look every key up.
-template <int D, int GT, bool kPaged, bool kHalfBlocks, bool kE4M3, int kWaves>
+template <int D, int GT, bool kPaged, bool kHalfBlocks, bool kE4M3, int kWaves, int kHeads>
 __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const QuantDecodeParams p) {
   constexpr int KK = D / 32;                 // products over the head dim per 16 keys
   constexpr int kKL = D / 64;                // key loads of 16 bytes per lane and 16 keys
@@ -46,12 +46,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   constexpr int kDL = D / 16;                // value features per lane
   constexpr int kVW = kDL / 4;               // words of their codes
   constexpr int kVL = kTile / 4;             // value loads per lane and tile (4 rows each)
-  constexpr int KPB = kWaves * kTile;        // keys per workgroup per round of tiles
+  constexpr int kOwn = kWaves / kHeads;      // waves of a head
+  constexpr int KPB = kOwn * kTile;          // keys per round of tiles
   constexpr int P = D / 2;
-  constexpr int kQ = (GT * P + kWaves * kWave - 1) / (kWaves * kWave);   // query pairs per thread
+  constexpr int kQ = (GT * P + kOwn * kWave - 1) / (kOwn * kWave);   // query pairs per thread
   constexpr int kPS = kTile / 2 + 4;         // words per weight row in LDS, padded (decode.hip)
   typedef uint32_t vrow __attribute__((ext_vector_type(kVW)));
-  __shared__ __align__(16) uint16_t s_q[3 * GT][D + 8];
+  __shared__ __align__(16) uint16_t s_q[kHeads][3 * GT][D + 8];
   __shared__ __align__(16) uint32_t s_p[kWaves][kPRows][kPS];
   __shared__ float s_m[kWaves][GT];
   __shared__ float s_l[kWaves][GT];
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   // the caches, 71 without the order).
   constexpr bool kHalfLines = D == 64 && kPaged;
   int kvh = blockIdx.x, row_y = blockIdx.y;
-  if constexpr (kHalfLines) {
+  if constexpr (kHalfLines && kHeads == 1) {
     const uint32_t id = blockIdx.x + gridDim.x * blockIdx.y, heads = gridDim.x;
     if (heads % 2 == 0 && id < heads * gridDim.y / 16 * 16) {
       const uint32_t pair = id / 16 * 8 + id % 8;
@@ -73,16 +74,18 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   }
   const int split = blockIdx.z;
   const int lane = threadIdx.x & (kWave - 1);
-  const double inv = p.inv_freq[threadIdx.x % P];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int head = wave / kOwn, thread = threadIdx.x - head * kOwn * kWave;   // of the workgroup's heads, and in its waves
+  kvh = kvh * kHeads + head;
+  const double inv = p.inv_freq[thread % P];
   int len_in;
   const int b = sequence_of_row<kWaves>(p, lane, row_of(p, split, row_y), &len_in);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n16 = lane % 16;                 // product column; operand row
   const int kj = lane / 16;                  // k group of the operands; head of the lane's scores
   const int G = p.group;
 
   const int len = clamp_len(p, kPaged, len_in);
-  if (len != len_in && split == 0 && kvh == 0 && threadIdx.x == 0 && p.err != nullptr)
+  if (len != len_in && split == 0 && kvh == 0 && thread == 0 && p.err != nullptr)
     atomicOr(p.err, PRCR_DERR_CAPACITY);
   const int chunk = chunk_keys(p, len);
   const int j0 = static_cast<int>(min(static_cast<int64_t>(len), static_cast<int64_t>(split) * chunk));
@@ -94,8 +97,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   float q_lo[kQ], q_hi[kQ];
 #pragma unroll
   for (int u = 0; u < kQ; ++u) {
-    const int g = u * (kWaves * kWave / P) + threadIdx.x / P;
-    const int64_t row = (static_cast<int64_t>(b) * p.n_q_heads + kvh * G + (g < G ? g : 0)) * D + threadIdx.x % P;
+    const int g = u * (kOwn * kWave / P) + thread / P;
+    const int64_t row = (static_cast<int64_t>(b) * p.n_q_heads + kvh * G + (g < G ? g : 0)) * D + thread % P;
     if (p.q_f32) {
       q_lo[u] = static_cast<const float *>(p.q)[row];
       q_hi[u] = static_cast<const float *>(p.q)[row + P];
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
 
   // The wave's tiles start at jw + n * KPB; the next tile's key rows are loaded once this tile's
   // products have read them, and its value rows once the value product has.
-  const int jw = j0 + wave * kTile;
+  const int jw = j0 + wave % kOwn * kTile;
   u32x4 kr[2][kKL];
   vrow vv[kVL];
   Entry e_next;
@@ -244,20 +247,20 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   // Turned, scaled query of every head of the group, in float32, as three bf16 parts in LDS.
   {
     const double qs = static_cast<double>(p.scale) * kLog2e;
-    const int i = threadIdx.x % P;
+    const int i = thread % P;
     double sn, cs;
     turn(static_cast<double>(q_pos) * inv, &sn, &cs);
 #pragma unroll
     for (int u = 0; u < kQ; ++u) {
-      const int g = u * (kWaves * kWave / P) + threadIdx.x / P;
+      const int g = u * (kOwn * kWave / P) + thread / P;
       if (g < GT) {
         const double x = q_lo[u], xp = q_hi[u];
         const float y = static_cast<float>((x * cs - xp * sn) * qs);
         const float yp = static_cast<float>((xp * cs + x * sn) * qs);
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
-          s_q[3 * g + part][i] = static_cast<uint16_t>(split_part(y, part) >> 16);
-          s_q[3 * g + part][i + P] = static_cast<uint16_t>(split_part(yp, part) >> 16);
+          s_q[head][3 * g + part][i] = static_cast<uint16_t>(split_part(y, part) >> 16);
+          s_q[head][3 * g + part][i + P] = static_cast<uint16_t>(split_part(yp, part) >> 16);
         }
       }
     }
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
   u32x4 qa[kA][KK];
 #pragma unroll
   for (int a = 0; a < kA; ++a) {
-    const uint16_t *row = s_q[3 * (4 * a + n16 / 4) + min(n16 % 4, 2)];
+    const uint16_t *row = s_q[head][3 * (4 * a + n16 / 4) + min(n16 % 4, 2)];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
       qa[a][kk] = *reinterpret_cast<const u32x4 *>(row + 16 * (kj + 4 * (kk / 2)) + 8 * (kk % 2));
@@ -437,18 +440,31 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const Q
           f32x4{acc[4 * c][r], acc[4 * c + 1][r], acc[4 * c + 2][r], acc[4 * c + 3][r]};
   }
   __syncthreads();
-  finish_split<kWaves, D, GT, GT == 4 ? 3 : 2, GT>(p, b, kvh, G, split, s_m, s_l, s_o);
+  finish_split<kOwn, D, GT, GT == 4 ? 3 : 2, GT>(p, b, kvh, G, split, thread,
+                                                 *reinterpret_cast<const float(*)[kOwn][GT]>(&s_m[head * kOwn]),
+                                                 *reinterpret_cast<const float(*)[kOwn][GT]>(&s_l[head * kOwn]),
+                                                 *reinterpret_cast<const float(*)[kOwn][16][D]>(&s_o[head * kOwn]));
 }
 
 template <int D, int GT, bool kE4M3, int kWaves>
 void launch_one(const QuantDecodeParams &p, bool paged, hipStream_t stream) {
-  const dim3 grid(p.n_kv_heads, p.batch, p.n_split), block(kWaves * kWave);
+  const dim3 grid(p.n_kv_heads / p.heads, p.batch, p.n_split), block(kWaves * kWave);
+  const bool halves = paged && p.block_size % 16 == 0;
+  if constexpr (D == 128 && kWaves == 4) {
+    if (p.heads == 2) {
+      if (halves)
+        quant_decode_kernel<D, GT, true, true, kE4M3, kWaves, 2><<<grid, block, 0, stream>>>(p);
+      else
+        quant_decode_kernel<D, GT, true, false, kE4M3, kWaves, 2><<<grid, block, 0, stream>>>(p);
+      return;
+    }
+  }
   if (!paged)
-    quant_decode_kernel<D, GT, false, false, kE4M3, kWaves><<<grid, block, 0, stream>>>(p);
-  else if (p.block_size % 16 == 0)
-    quant_decode_kernel<D, GT, true, true, kE4M3, kWaves><<<grid, block, 0, stream>>>(p);
+    quant_decode_kernel<D, GT, false, false, kE4M3, kWaves, 1><<<grid, block, 0, stream>>>(p);
+  else if (halves)
+    quant_decode_kernel<D, GT, true, true, kE4M3, kWaves, 1><<<grid, block, 0, stream>>>(p);
   else
-    quant_decode_kernel<D, GT, true, false, kE4M3, kWaves><<<grid, block, 0, stream>>>(p);
+    quant_decode_kernel<D, GT, true, false, kE4M3, kWaves, 1><<<grid, block, 0, stream>>>(p);
 }
 
 template <int D, int GT>
@@ -462,21 +478,30 @@ void launch_code(const QuantDecodeParams &p, prcr_code code, bool paged, hipStre
 // How a call is split, within the room for decode_splits' partials (p->n_split on entry).  As decode.hip's
 // plan, only the sequence's length and the call's shape enter, and half the bytes a key move its borders:
 //   - a cache of at most 1,024 slots (head_dim 64: 2,048) is one chunk a sequence: 8 sequences of 400-800
-//     keys, 8 KV heads, take 9.7 us so, in chunks and a merge 10.4; one of 1,152 keys 10.2 and 9.9;
-//   - else one workgroup per compute unit, and two to four, of 1,024 keys and more, where there are several
+//     keys, 8 KV heads, take 9.4 us so, in chunks and a merge 10.4; one of 1,152 keys 10.2 and 9.9;
+//   - else one workgroup per compute unit (head_dim 64: two; 8 sequences of 8,000 keys, 8 heads, 19.8 us with
+//     eight chunks each, 23.3 with four), and two to four, of 1,024 keys and more, where there are several
 //     sequences, which may differ in length: 64 of 2,912-6,512 keys, 4 KV heads, 62 us in two chunks and 69 in one
 //     (32 of 2,756-4,256, 8 KV heads, 41 and 40; one of 120,001 42 in 32 and 43 in 64; 64 of
 //     1,000-2,000, 4 KV heads, 25 in two and 23 in one).
 // A sequence that is one chunk is read by eight waves where they are few, or have half the bytes a key
 // (one of 600 keys: 7.7 us, with four waves 8.1; 32 of 1,000-2,000, 8 heads of 64: 11.7 and 14.3; but 64
 // of 1,000-2,000, 4 heads of 128, 24.1 and 23.0).  More than about 42 GB/s a compute unit does not read.
+//
+// Paged rows of one head are 128 bytes here and there.  With 8 heads and more a workgroup takes two
+// neighbouring ones, 256 bytes of a slot at about the same time: 16 sequences of 3,000-5,000 keys, 8
+// heads, 31.3 us with one and 29.1 with two, 64 of 1,500-3,000 62.6 and 55.5 (contiguous: 25.0 with one,
+// 25.8 with two; 64 of 2,912-6,512 keys, 4 heads, 62 either way; four heads are no better than two).
 void plan(QuantDecodeParams *p, int head_dim, bool paged) {
-  const int64_t room = p->n_split, pairs = static_cast<int64_t>(p->batch) * p->n_kv_heads;
   const int64_t capacity = paged ? static_cast<int64_t>(p->max_blocks) * p->block_size : p->s_max;
+  const bool direct = capacity <= (head_dim == 64 ? 2048 : 1024);
+  p->heads = !direct && paged && head_dim == 128 && p->n_kv_heads >= 8 && p->n_kv_heads % 2 == 0 ? 2 : 1;
+  const int64_t room = p->n_split, pairs = static_cast<int64_t>(p->batch) * p->n_kv_heads / p->heads;
   constexpr int kMinKeys = 1024;
   int64_t fill = 1, n = 1;
-  if (capacity > (head_dim == 64 ? 2048 : 1024)) {
-    fill = pairs >= 3 * kUnits / 4 ? 1 : splits_in_rounds(pairs, 3 * kUnits / 4, 2 * kUnits, room, 0.9);
+  if (!direct) {
+    const int64_t units = head_dim == 64 ? 2 * kUnits : kUnits;
+    fill = pairs >= 3 * units / 4 ? 1 : splits_in_rounds(pairs, 3 * units / 4, 2 * units, room, 0.9);
     n = fill;
     if (p->batch > 1 && capacity / kMinKeys >= std::min(ceil_div(2 * kUnits, pairs), room)) {
       const int64_t more = splits_in_rounds(pairs, 2 * kUnits, 4 * kUnits, room, 0.9);
@@ -486,8 +511,8 @@ void plan(QuantDecodeParams *p, int head_dim, bool paged) {
   p->n_split = static_cast<int32_t>(n);
   p->fill = static_cast<int32_t>(fill);
   p->min_keys = kMinKeys / 2;                // (of a chunk of a shorter sequence)
-  p->waves = n == 1 && (head_dim == 64 || pairs <= kUnits / 2) ? 8 : 4;
-  p->round = p->waves * kTile;
+  p->waves = n == 1 && p->heads == 1 && (head_dim == 64 || pairs <= kUnits / 2) ? 8 : 4;
+  p->round = p->waves / p->heads * kTile;
   auto inverse = [](int64_t m) { return m > 1 ? static_cast<uint32_t>(((int64_t{1} << 32) + m - 1) / m) : 0u; };
   p->split_inverse = inverse(n);
   p->fill_inverse = inverse(fill);
