@@ -928,6 +928,8 @@ def quant_append(rope: Rope, cache: QuantCache, layer: int, raw_k, raw_v, pos, n
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B = _batch(cache)
+    if rope.head_dim != D:
+        raise ValueError("rope head_dim differs from the cache's")
     _need(raw_k, "raw_k", None, 4, cache.device)
     _need(raw_v, "raw_v", raw_k.dtype, 4, cache.device)
     dtype = _dtype_code(raw_k)
@@ -941,9 +943,10 @@ def quant_append(rope: Rope, cache: QuantCache, layer: int, raw_k, raw_v, pos, n
     _need(cache_start, "cache_start", torch.int32, 1, cache.device)
     _shape(cache_start, "cache_start", (B,))
     _err(err, cache.device)
-    st = lib().prcr_quant_append(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL),
-                                 int(H), layer, _ptr(raw_k), _ptr(raw_v), S, _ptr(pos), _ptr(n_tokens),
-                                 _ptr(cache_start), _ptr(err), _stream(stream, cache.device))
+    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
+        st = lib().prcr_quant_append(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL),
+                                     int(H), layer, _ptr(raw_k), _ptr(raw_v), S, _ptr(pos), _ptr(n_tokens),
+                                     _ptr(cache_start), _ptr(err), _stream(stream, cache.device))
     _check("prcr_quant_append", st)
 
 
@@ -975,10 +978,11 @@ def quant_rebind_inject(rope: Rope, mem: Memory, sel_off, sel_idx, new_pos, cach
     _shape(new_cache_len, "new_cache_len", (B,))
     _shape(slot_mapping, "slot_mapping", (total_k,))
     _err(err, mem.device)
-    st = lib().prcr_quant_rebind_inject(
-        ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(new_pos),
-        ctypes.byref(cache.to_c()), _ptr(cache_len), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
-        _stream(stream, mem.device))
+    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
+        st = lib().prcr_quant_rebind_inject(
+            ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(new_pos),
+            ctypes.byref(cache.to_c()), _ptr(cache_len), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
+            _stream(stream, mem.device))
     _check("prcr_quant_rebind_inject", st)
     return new_cache_len, slot_mapping
 
@@ -1008,8 +1012,9 @@ def quant_read(cache: QuantCache, layer: int, cache_len, dtype, k=None, v=None, 
     _shape(k, "k", shape)
     _shape(v, "v", shape)
     _err(err, cache.device)
-    st = lib().prcr_quant_read(ctypes.byref(cache.to_c()), _dtype_code(k), int(B), int(NL), int(H), int(D), layer,
-                               _ptr(cache_len), _ptr(k), _ptr(v), S, _ptr(err), _stream(stream, cache.device))
+    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
+        st = lib().prcr_quant_read(ctypes.byref(cache.to_c()), _dtype_code(k), int(B), int(NL), int(H), int(D), layer,
+                                   _ptr(cache_len), _ptr(k), _ptr(v), S, _ptr(err), _stream(stream, cache.device))
     _check("prcr_quant_read", st)
     return k, v
 
@@ -1033,6 +1038,8 @@ def quant_decode_attention(rope: Rope, cache: QuantCache, layer: int, q, q_pos, 
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B = _batch(cache)
+    if rope.head_dim != D:
+        raise ValueError("rope head_dim differs from the cache's")
     _need(q, "q", None, 3, cache.device)
     dtype = _dtype_code(q)
     Hq = q.shape[1]
@@ -1048,9 +1055,10 @@ def quant_decode_attention(rope: Rope, cache: QuantCache, layer: int, q, q_pos, 
     workspace = _workspace(workspace, quant_decode_workspace_bytes(cache, Hq), cache.device, stream)
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
-    st = lib().prcr_quant_decode_attention(
-        ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL), int(H), layer, _ptr(q), int(Hq),
-        _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
+    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
+        st = lib().prcr_quant_decode_attention(
+            ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL), int(H), layer, _ptr(q), int(Hq),
+            _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
     _check("prcr_quant_decode_attention", st)
     return out

@@ -24,6 +24,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/StreamGuard.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Device.h>
@@ -751,7 +752,7 @@ PyObject *quant_append(Args a) {
   const int32_t layer = int32_of(a[2]);
   const at::Tensor raw_k = tensor(a[3]), raw_v = tensor(a[4]), pos = tensor(a[5]), n_tokens = tensor(a[6]),
                    start = tensor(a[7]);
-  if (raw_k.dim() != 4) throw Skip();
+  if (raw_k.dim() != 4 || rope.head_dim != cache.head_dim) throw Skip();
   const prcr_dtype dtype = dtype_of(raw_k);
   const int64_t B = cache.batch, S = raw_k.size(1);
   const at::DimVector shape{B, S, cache.n_kv_heads, cache.head_dim};
@@ -766,6 +767,7 @@ PyObject *quant_append(Args a) {
   prcr_status st;
   {
     Unlocked u;
+    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     st = prcr_quant_append(&rope, &cache.c, dtype, cache.batch, cache.n_layers, cache.n_kv_heads, layer, ptr<void>(raw_k),
                            ptr<void>(raw_v), s_src, ptr<int32_t>(pos), ptr<int32_t>(n_tokens), ptr<int32_t>(start),
                            ptr<int32_t>(err), on.handle());
@@ -792,6 +794,7 @@ PyObject *quant_rebind_inject(Args a) {
   prcr_status st;
   {
     Unlocked u;
+    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     new_len.make(on);
     slots.make(on);
     st = prcr_quant_rebind_inject(&rope, &m.c, ptr<int32_t>(sel.off), ptr<int32_t>(sel.idx), sel.k, ptr<double>(new_pos),
@@ -820,6 +823,7 @@ PyObject *quant_read(Args a) {
   prcr_status st;
   {
     Unlocked u;
+    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     k.make(on);
     v.make(on);
     st = prcr_quant_read(&cache.c, dtype_of(k.t), cache.batch, cache.n_layers, cache.n_kv_heads, cache.head_dim, layer,
@@ -835,7 +839,7 @@ PyObject *quant_decode_attention(Args a) {
   const QuantStore cache(a[1]);
   const int32_t layer = int32_of(a[2]);
   const at::Tensor q = tensor(a[3]), q_pos = tensor(a[4]), cache_len = tensor(a[5]);
-  if (q.dim() != 3) throw Skip();
+  if (q.dim() != 3 || rope.head_dim != cache.head_dim) throw Skip();
   const prcr_dtype dtype = dtype_of(q);
   const int64_t B = cache.batch, Hq = q.size(1), D = cache.head_dim;
   need(q, q.scalar_type(), cache.device, {B, Hq, D});
@@ -853,6 +857,7 @@ PyObject *quant_decode_attention(Args a) {
   prcr_status st;
   {
     Unlocked u;
+    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     out.make(on);
     ws.make(on);
     st = prcr_quant_decode_attention(&rope, &cache.c, dtype, cache.batch, cache.n_layers, cache.n_kv_heads, layer,

@@ -39,6 +39,10 @@ SHAPES = {
     "three": (5, 3, [90], 2100),
     "long": (1, 6, [5000], 5001),
     "roomy": (2, 4, [40, 1100], 9000),
+    "pairs of heads": (8, 4, [1100, 40, 0, 900], 1200),
+    "ten heads": (10, 3, [2100], 2150),
+    "many rows": (4, 2, [33, 0, 64, 200, 1, 130, 299, 300], 300),
+    "odd rows": (6, 1, [90, 7, 250], 2500),
 }
 
 
@@ -68,6 +72,22 @@ def test_many_sequences():
         out, err = run(rope, store.to(DEV), 0, *x)
         assert err == 0
         check_attention(out, attention(rope, store, 0, *x, 0.125))
+
+
+@pytest.mark.parametrize("block", [0, 16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_several_chunks_of_sequences_that_differ(D, block):
+    """Enough pairs of sequence and head for two rounds of workgroups over the chip, lengths from none to the
+    capacity."""
+    print(f"quant decode, chunks of many sequences, D={D} block={block}", flush=True)
+    rng = np.random.default_rng(D + block)
+    lens = np.concatenate([[0, 1, 2100, 1023, 1024, 1025], rng.integers(2, 2100, 26)])
+    store = Store(torch.int8, 32, 1, 8, D, 2100, block, seed=1).fill(seed=1)
+    x = inputs("bf16", D, 8, 1, lens, seed=2)
+    rope = prcr.Rope(*ROPES[D])
+    out, err = run(rope, store.to(DEV), 0, *x)
+    assert err == 0
+    check_attention(out, attention(rope, store, 0, *x, D ** -0.5))
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.3, 4.0])
