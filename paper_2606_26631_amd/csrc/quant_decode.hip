@@ -9,6 +9,11 @@
 // are split into three bf16 parts whose sum they are, so that the products are exact and their
 // sums float32.  The key's scale multiplies the score, and the value's the weight before it is
 // split: neither costs an operation per element.
+//
+// What bounds it is reading the cache: 32 sequences of 2,756-4,256 keys, 8 heads, 237 MB, take 38 us at
+// 6.2 TB/s and 4.7 in the merge, 64 paged ones of 2,912-6,512 in int8, 4 heads, 319 MB, 58.9 (5.4 TB/s) and
+// 4.8.  Eight codes a lane on the vector ALU, with the scores summed across lanes, took 115 and 383.
+// int8 keys multiplied as integers, with the query in four digits, were no faster (61.8 and 61.7 us a call).
 #include <algorithm>
 #include <type_traits>
 
@@ -18,8 +23,6 @@
 
 namespace prcr {
 namespace {
-
-typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
 
 // Two codes of a word (its lower or upper half) as two bf16 numbers.
 template <bool kE4M3, bool kUpper>
@@ -36,6 +39,7 @@ __device__ __forceinline__ uint32_t codes2(uint32_t w) {
 // GT: query heads per KV head there is room for (4 or 8; smaller groups repeat their first head).
 // kHalfBlocks (paged only): block_size is a multiple of 16, so that each half of a tile (tiles
 // start at multiples of 32) lies in one block; other block sizes look every key up.
+// kHeads: KV heads of a workgroup, whose waves are shared out to them (plan).
 template <int D, int GT, bool kPaged, bool kHalfBlocks, bool kE4M3, int kWaves, int kHeads>
 __global__ __launch_bounds__(kWaves * kWave, 2) void quant_decode_kernel(const QuantDecodeParams p) {
   constexpr int KK = D / 32;                 // products over the head dim per 16 keys
