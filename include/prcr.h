@@ -502,12 +502,13 @@ prcr_status prcr_evict_workspace_size(const prcr_cache *cache, int32_t batch,
  * values as they are) and Q the largest code, 448 or 127, all in float32:
  *   scale = max(max |x_i| / Q, 2^-126),   code_i = nearest(x_i (1 / scale)), ties to even
  * so that code_i scale is within 2^-4 of x_i relative to it or 2^-10 scale (E4M3), or within scale / 2
- * (I8), each but for float32's roundings.  A row with an infinity or a NaN gets codes 0 and scale NaN: all of it reads back
- * as NaN.
+ * (I8), each but for float32's roundings.  (Of the finite numbers the largest float32 alone reads back as an
+ * infinity, in I8, where 127 scale rounds to one.)  A row with an infinity or a NaN gets codes 0 and
+ * scale NaN: all of it reads back as NaN.
  *
- * Every array that a call writes must share no memory with another one (PRCR_ERR_ALIAS).  head_dim 64 or 128 and the
- * axis maps of prcr_rebind_inject; the capacity per sequence (s_max, or max_blocks * block_size) at
- * most 2^30 slots, batch and n_kv_heads at most 65535, else PRCR_ERR_SHAPE.
+ * Every array that a call writes must share no memory with another one (PRCR_ERR_ALIAS).  head_dim 64
+ * or 128 and the axis maps of prcr_rebind_inject; the capacity per sequence (s_max, or
+ * max_blocks * block_size) at most 2^30 slots, batch and n_kv_heads at most 65535, else PRCR_ERR_SHAPE.
  */
 typedef enum prcr_code PRCR_ENUM_BASE {
   PRCR_E4M3 = 0,               /* 8-bit float, 4 exponent and 3 fraction bits, no infinities */

@@ -357,3 +357,28 @@ def test_a_row_revisited_where_it_was_appended_has_the_same_codes():
         torch.cuda.synchronize()
         for t in (cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale):
             assert torch.equal(t[:, :, :, :20], t[:, :, :, 20:40])
+
+
+@pytest.mark.parametrize("kind", sorted(CODES))
+def test_the_largest_numbers(kind):
+    """Rows whose largest magnitude is among the type's last 64: codes and scales bit for bit, and read back finite but
+    for int8's largest float32, whose 127 scale rounds to an infinity."""
+    print(f"the largest numbers {kind}", flush=True)
+    D = 128
+    x = np.tile(np.linspace(-1, 1, D, dtype=np.float32), (64, 1))
+    x[:, 5] = np.arange(0x7F7FFFFF - 63, 0x7F800000, dtype=np.uint32).view(np.float32)
+    store = Store(CODES[kind], 1, 1, 1, D, 64)
+    cache, err = store.to(DEV), error()
+    raw = torch.from_numpy(x).view(1, 64, 1, D).to(DEV)
+    length = to_dev(np.array([64], np.int32))
+    prcr.quant_append(prcr.Rope(*ROPES[D][0]), cache, 0, raw, raw, torch.zeros(1, 64, 3, dtype=torch.int32, device=DEV), length,
+                      to_dev(np.array([0], np.int32)), err=err)
+    k, v = prcr.quant_read(cache, 0, length, torch.float32)
+    code, scale = quantised32(x, CODES[kind])
+    got = store.take(cache)
+    for name, t in (("k", k), ("v", v)):
+        c, s = got.rows(name, 0, np.arange(64))
+        assert np.array_equal(s[:, 0, 0].view(np.int32), scale.view(np.int32)) and np.array_equal(c[:, 0, 0], code)
+        finite = t[0, 0, 0].isfinite().cpu().numpy()
+        assert finite[:63].all() and np.array_equal(~finite[63], (np.arange(D) == 5) & (kind == "i8"))
+    assert int(err.item()) == 0
