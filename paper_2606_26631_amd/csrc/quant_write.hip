@@ -176,14 +176,15 @@ __global__ __launch_bounds__(kWaves * kWave) void quant_write_kernel(const Quant
 #pragma unroll
     for (int a = 0; a < 3; ++a) pos[a] = p.new_pos[3 * static_cast<int64_t>(t) + a];
     // The last sequence that begins at or before t.  Fewer than 64 sequences' offsets are held by the
-    // wave's lanes, one each.
+    // wave's lanes, one each; all lanes take part in every shuffle, whatever their own `at` is (one that
+    // were switched off would be read as 0).
     int s0, s1, last = 0;
     if (p.batch < kWave) {
       const int held = p.sel_off[min(lane, p.batch)];
 #pragma unroll
       for (int step = 32; step > 0; step >>= 1) {
-        const int at = last + step;
-        last = at <= p.batch && __shfl(held, at & 63) <= t ? at : last;
+        const int at = last + step, begins = __shfl(held, at & 63);
+        last = at <= p.batch && begins <= t ? at : last;
       }
       b = min(last, p.batch - 1);
       s0 = __shfl(held, b);
