@@ -633,6 +633,12 @@ def _cache_dims(cache: Cache):
     return NL, H, D
 
 
+def _rope_matches(rope: Rope, head_dim):
+    """The C calls on a cache take the length of its rows from the rope."""
+    if rope.head_dim != head_dim:
+        raise ValueError("rope head_dim differs from the cache's")
+
+
 def decode_workspace_bytes(cache: Cache, batch: int, n_q_heads: int) -> int:
     """Bytes of workspace prcr_decode_attention needs (prcr_decode_workspace_size)."""
     NL, H, D = _cache_dims(cache)
@@ -654,6 +660,7 @@ def decode_attention(rope: Rope, cache: Cache, layer: int, q, q_pos, cache_len, 
     layer = _int32(layer, "layer")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
+    _rope_matches(rope, D)
     _need(q, "q", cache.k.dtype, 3, cache.device)
     B, Hq = q.shape[0], q.shape[1]
     if q.shape[2] != D:
@@ -700,6 +707,7 @@ def decode_attention_static(rope: Rope, cache: Cache, layer: int, q, q_pos, cach
     layer = _int32(layer, "layer")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
+    _rope_matches(rope, D)
     _need(q, "q", cache.k.dtype, 3, cache.device)
     B, Hq = q.shape[0], q.shape[1]
     if q.shape[2] != D:
@@ -752,10 +760,11 @@ def _workspace(workspace, need, device, stream):
     return workspace
 
 
-def _query_rows(cache: Cache, q, q_off, q_pos, cache_len, q_len):
+def _query_rows(rope: Rope, cache: Cache, q, q_off, q_pos, cache_len, q_len):
     """Checks of the packed query rows; (batch, rows, query heads)."""
     torch = _torch()
     NL, H, D = _cache_dims(cache)
+    _rope_matches(rope, D)
     _need(q, "q", cache.k.dtype, 3, cache.device)
     T, Hq = q.shape[0], q.shape[1]
     if q.shape[2] != D:
@@ -795,7 +804,7 @@ def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache
     layer = _int32(layer, "layer")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
-    B, T, Hq = _query_rows(cache, q, q_off, q_pos, cache_len, q_len)
+    B, T, Hq = _query_rows(rope, cache, q, q_off, q_pos, cache_len, q_len)
     if out is None:
         out = _new((T, Hq, D), cache.k.dtype, cache.device, stream)
     if lse is None:
@@ -839,7 +848,7 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
     window = None if window is None else _int32(window, "window")
     torch = _torch()
     NL, H, D = _cache_dims(cache)
-    B, T, Hq = _query_rows(cache, q, q_off, q_pos, cache_len, q_len)
+    B, T, Hq = _query_rows(rope, cache, q, q_off, q_pos, cache_len, q_len)
     _need(lse, "lse", torch.float32, 2, cache.device)
     _shape(lse, "lse", (T, Hq))
     if window is not None and window < 1:
@@ -928,8 +937,7 @@ def quant_append(rope: Rope, cache: QuantCache, layer: int, raw_k, raw_v, pos, n
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B = _batch(cache)
-    if rope.head_dim != D:
-        raise ValueError("rope head_dim differs from the cache's")
+    _rope_matches(rope, D)
     _need(raw_k, "raw_k", None, 4, cache.device)
     _need(raw_v, "raw_v", raw_k.dtype, 4, cache.device)
     dtype = _dtype_code(raw_k)
@@ -1038,8 +1046,7 @@ def quant_decode_attention(rope: Rope, cache: QuantCache, layer: int, q, q_pos, 
     torch = _torch()
     NL, H, D = _cache_dims(cache)
     B = _batch(cache)
-    if rope.head_dim != D:
-        raise ValueError("rope head_dim differs from the cache's")
+    _rope_matches(rope, D)
     _need(q, "q", None, 3, cache.device)
     dtype = _dtype_code(q)
     Hq = q.shape[1]

@@ -556,7 +556,7 @@ PyObject *decode(Args a) {
   const Store cache(a[1]);
   const int32_t layer = int32_of(a[2]);
   const at::Tensor q = tensor(a[3]), q_pos = tensor(a[4]), cache_len = tensor(a[5]);
-  if (q.dim() != 3) throw Skip();
+  if (q.dim() != 3 || rope.head_dim != cache.k.size(4)) throw Skip();
   const int64_t B = q.size(0), Hq = q.size(1), D = cache.k.size(4);
   need(q, cache.k.scalar_type(), cache.device, {B, Hq, D});
   if (cache.rows() != B) throw Skip();
@@ -600,9 +600,10 @@ PyObject *decode(Args a) {
 // The packed query rows of the operators on several tokens per sequence:
 // (q, q_off, q_pos, cache_len, q_len)
 struct QueryRows {
-  QueryRows(const Store &cache, PyObject *q_, PyObject *off_, PyObject *pos_, PyObject *len_, PyObject *rows_)
+  QueryRows(const prcr_rope &rope, const Store &cache, PyObject *q_, PyObject *off_, PyObject *pos_, PyObject *len_,
+            PyObject *rows_)
       : q(tensor(q_)), off(tensor(off_)), pos(tensor(pos_)), cache_len(tensor(len_)), len(tensor_or_none(rows_)) {
-    if (q.dim() != 3) throw Skip();
+    if (q.dim() != 3 || rope.head_dim != cache.k.size(4)) throw Skip();
     need(q, cache.k.scalar_type(), cache.device, {q.size(0), q.size(1), cache.k.size(4)});
     need(off, at::kInt, cache.device, {cache.rows() + 1});
     need(pos, at::kInt, cache.device, {q.size(0), 3});
@@ -639,7 +640,7 @@ PyObject *chunk_attention(Args a) {
   const prcr_rope rope = rope_of(a[0]);
   const Store cache(a[1]);
   const int32_t layer = int32_of(a[2]);
-  const QueryRows rows(cache, a[3], a[4], a[5], a[6], a[7]);
+  const QueryRows rows(rope, cache, a[3], a[4], a[5], a[6], a[7]);
   const int64_t T = rows.total, Hq = rows.heads, D = cache.k.size(4);
   const double scale = a[8] == Py_None ? std::pow(static_cast<double>(D), -0.5) : double_of(a[8]);
   Out out(a[9], cache.k.scalar_type(), cache.device, {T, Hq, D}), lse(a[10], at::kFloat, cache.device, {T, Hq});
@@ -672,7 +673,7 @@ PyObject *key_weights(Args a) {
   const prcr_rope rope = rope_of(a[0]);
   const Store cache(a[1]);
   const int32_t layer = int32_of(a[2]);
-  const QueryRows rows(cache, a[3], a[4], a[5], a[6], a[8]);
+  const QueryRows rows(rope, cache, a[3], a[4], a[5], a[6], a[8]);
   const at::Tensor lse = tensor(a[7]);
   const int64_t T = rows.total, Hq = rows.heads, D = cache.k.size(4);
   need(lse, at::kFloat, cache.device, {T, Hq});
