@@ -222,6 +222,14 @@ def _stream(stream, device):
     return c_void_p(s.cuda_stream)
 
 
+def _launch(fn, device, stream, *args):
+    """The C call fn on `stream`, or on the current one of `device`, which is the current device meanwhile:
+    torch's default stream has no number of its own, and stands for the current device's."""
+    with _torch().cuda.device(device):
+        status = getattr(lib(), fn)(*args, _stream(stream, device))
+    _check(fn, status)
+
+
 def _new(shape, dtype, device, stream, given=True):
     """Memory made for a call on `stream`.  On another stream than torch's current one it is
     that stream's: a block of the current stream's might still be read there when the kernels
@@ -456,10 +464,8 @@ def store_raw(mem: Memory, layer: int, raw_k, raw_v, vis_rows, err=None, stream=
     if tuple(vis_rows.shape) != (B, M):
         raise ValueError("vis_rows must be [B, M_max]")
     _err(err, mem.device)
-    st = lib().prcr_store_raw(ctypes.byref(mem.to_c()), layer, _ptr(raw_k), _ptr(raw_v),
-                              int(raw_k.shape[1]), _ptr(vis_rows), _ptr(err),
-                              _stream(stream, mem.device))
-    _check("prcr_store_raw", st)
+    _launch("prcr_store_raw", mem.device, stream, ctypes.byref(mem.to_c()), layer, _ptr(raw_k), _ptr(raw_v),
+            int(raw_k.shape[1]), _ptr(vis_rows), _ptr(err))
 
 
 def reassign_coords(mem: Memory, sel_off, sel_idx, p_txt, mode: str = "pcr", l_ext: int = 2,
@@ -489,10 +495,8 @@ def reassign_coords(mem: Memory, sel_off, sel_idx, p_txt, mode: str = "pcr", l_e
     _err(err, mem.device)
     if mode not in MODES:
         raise ValueError(f"mode must be one of {sorted(MODES)}")
-    st = lib().prcr_reassign_coords(ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx), total_k,
-                                    _ptr(p_txt), MODES[mode], l_ext, _ptr(new_pos),
-                                    _ptr(next_pos), _ptr(err), _stream(stream, mem.device))
-    _check("prcr_reassign_coords", st)
+    _launch("prcr_reassign_coords", mem.device, stream, ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx),
+            total_k, _ptr(p_txt), MODES[mode], l_ext, _ptr(new_pos), _ptr(next_pos), _ptr(err))
     return new_pos, next_pos
 
 
@@ -523,11 +527,9 @@ def rebind_inject(rope: Rope, mem: Memory, sel_off, sel_idx, new_pos, cache: Cac
     _no_alias([(("new_cache_len", new_cache_len), ("cache_len", cache_len)),
                (("new_cache_len", new_cache_len), ("sel_off", sel_off))])
     _err(err, mem.device)
-    st = lib().prcr_rebind_inject(ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off),
-                                  _ptr(sel_idx), total_k, _ptr(new_pos), ctypes.byref(cache.to_c()),
-                                  _ptr(cache_len), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
-                                  _stream(stream, mem.device))
-    _check("prcr_rebind_inject", st)
+    _launch("prcr_rebind_inject", mem.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()),
+            _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(new_pos), ctypes.byref(cache.to_c()), _ptr(cache_len),
+            _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err))
     return new_cache_len, slot_mapping
 
 
@@ -581,12 +583,9 @@ def revisit(rope: Rope, mem: Memory, sel_off, sel_idx, p_txt, cache: Cache, cach
     _err(err, mem.device)
     if mode not in MODES:
         raise ValueError(f"mode must be one of {sorted(MODES)}")
-    st = lib().prcr_revisit(ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off),
-                            _ptr(sel_idx), total_k, _ptr(p_txt), MODES[mode], l_ext,
-                            ctypes.byref(cache.to_c()), _ptr(cache_len), _ptr(new_pos),
-                            _ptr(next_pos), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
-                            _stream(stream, mem.device))
-    _check("prcr_revisit", st)
+    _launch("prcr_revisit", mem.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()),
+            _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(p_txt), MODES[mode], l_ext, ctypes.byref(cache.to_c()),
+            _ptr(cache_len), _ptr(new_pos), _ptr(next_pos), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err))
     return new_pos, next_pos, new_cache_len, slot_mapping
 
 
@@ -616,12 +615,9 @@ def prefill_capture(rope: Rope, mem: Memory, layer: int, raw_k, raw_v, pos, n_to
     _need(cache_start, "cache_start", torch.int32, 1, mem.device)
     _shape(cache_start, "cache_start", (B,))
     _err(err, mem.device)
-    st = lib().prcr_prefill_capture(ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), layer,
-                                    _ptr(raw_k), _ptr(raw_v), int(S), _ptr(pos), _ptr(n_tokens),
-                                    _ptr(vis_index), int(bool(write_coords)),
-                                    ctypes.byref(cache.to_c()), _ptr(cache_start), _ptr(err),
-                                    _stream(stream, mem.device))
-    _check("prcr_prefill_capture", st)
+    _launch("prcr_prefill_capture", mem.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()),
+            layer, _ptr(raw_k), _ptr(raw_v), int(S), _ptr(pos), _ptr(n_tokens), _ptr(vis_index),
+            int(bool(write_coords)), ctypes.byref(cache.to_c()), _ptr(cache_start), _ptr(err))
 
 
 def _cache_dims(cache: Cache):
@@ -681,16 +677,13 @@ def decode_attention(rope: Rope, cache: Cache, layer: int, q, q_pos, cache_len, 
     if workspace is None:
         workspace = _new(((max(need, 4) + 3) // 4,), torch.float32, cache.device, stream, given=False)
     _need(workspace, "workspace", None, None, cache.device)
-    if workspace.numel() * workspace.element_size() < need:
+    if workspace.nbytes < need:
         raise ValueError(f"workspace needs {need} bytes")
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
-    st = lib().prcr_decode_attention(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
-                                     _dtype_code(cache.k), int(B), int(NL), int(H), layer,
-                                     _ptr(q), int(Hq), _ptr(q_pos), _ptr(cache_len), sc, _ptr(out),
-                                     _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                     _ptr(err), _stream(stream, cache.device))
-    _check("prcr_decode_attention", st)
+    _launch("prcr_decode_attention", cache.device, stream, ctypes.byref(rope.to_c()),
+            ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H), layer, _ptr(q), int(Hq),
+            _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(workspace), workspace.nbytes, _ptr(err))
     return out
 
 
@@ -726,12 +719,9 @@ def decode_attention_static(rope: Rope, cache: Cache, layer: int, q, q_pos, cach
     _shape(out, "out", (B, Hq, D))
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
-    st = lib().prcr_decode_attention_static(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
-                                            _dtype_code(cache.k), int(B), int(NL), int(H),
-                                            layer, _ptr(q), int(Hq), _ptr(q_pos),
-                                            _ptr(cache_len), sc, _ptr(out), _ptr(err),
-                                            _stream(stream, cache.device))
-    _check("prcr_decode_attention_static", st)
+    _launch("prcr_decode_attention_static", cache.device, stream, ctypes.byref(rope.to_c()),
+            ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H), layer, _ptr(q), int(Hq),
+            _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(err))
     return out
 
 
@@ -755,7 +745,7 @@ def _workspace(workspace, need, device, stream):
     if workspace is None:
         return _new(((max(need, 4) + 3) // 4,), torch.float32, device, stream, given=False)
     _need(workspace, "workspace", None, None, device)
-    if workspace.numel() * workspace.element_size() < need:
+    if workspace.nbytes < need:
         raise ValueError(f"workspace needs {need} bytes")
     return workspace
 
@@ -816,12 +806,10 @@ def chunk_attention(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache
     workspace = _workspace(workspace, chunk_workspace_bytes(cache, T, Hq), cache.device, stream)
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
-    st = lib().prcr_chunk_attention(
-        ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H),
-        layer, _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len), sc,
-        _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err),
-        _stream(stream, cache.device))
-    _check("prcr_chunk_attention", st)
+    _launch("prcr_chunk_attention", cache.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
+            _dtype_code(cache.k), int(B), int(NL), int(H), layer, _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len),
+            int(T), _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(lse), _ptr(workspace), workspace.nbytes,
+            _ptr(err))
     return out, lse
 
 
@@ -862,13 +850,10 @@ def key_weights(rope: Rope, cache: Cache, layer: int, q, q_off, q_pos, cache_len
     workspace = _workspace(workspace, key_weights_workspace_bytes(cache, T, Hq, window), cache.device, stream)
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
-    st = lib().prcr_key_weights(
-        ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H),
-        layer, _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len), int(T), _ptr(q_pos), _ptr(cache_len),
-        _ptr(lse), 0 if window is None else window, sc, int(bool(accumulate)), _ptr(weights),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err),
-        _stream(stream, cache.device))
-    _check("prcr_key_weights", st)
+    _launch("prcr_key_weights", cache.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
+            _dtype_code(cache.k), int(B), int(NL), int(H), layer, _ptr(q), int(Hq), _ptr(q_off), _ptr(q_len),
+            int(T), _ptr(q_pos), _ptr(cache_len), _ptr(lse), 0 if window is None else window, sc,
+            int(bool(accumulate)), _ptr(weights), _ptr(workspace), workspace.nbytes, _ptr(err))
     return weights
 
 
@@ -915,12 +900,10 @@ def evict(cache: Cache, cache_len, weights, budget: int, keep_first: int = 0, ke
     _shape(new_weights, "new_weights", (B, H, cap))
     workspace = _workspace(workspace, evict_workspace_bytes(cache, budget), cache.device, stream)
     _err(err, cache.device)
-    st = lib().prcr_evict(
-        ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B), int(NL), int(H), int(D), _ptr(cache_len),
-        _ptr(weights), budget, keep_first, keep_last, _ptr(new_cache_len), _ptr(kept),
-        _ptr(new_weights), None if mem is None else ctypes.byref(mem.to_c()), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
-    _check("prcr_evict", st)
+    _launch("prcr_evict", cache.device, stream, ctypes.byref(cache.to_c()), _dtype_code(cache.k), int(B),
+            int(NL), int(H), int(D), _ptr(cache_len), _ptr(weights), budget, keep_first, keep_last,
+            _ptr(new_cache_len), _ptr(kept), _ptr(new_weights),
+            None if mem is None else ctypes.byref(mem.to_c()), _ptr(workspace), workspace.nbytes, _ptr(err))
     return new_cache_len, kept, new_weights
 
 
@@ -951,11 +934,9 @@ def quant_append(rope: Rope, cache: QuantCache, layer: int, raw_k, raw_v, pos, n
     _need(cache_start, "cache_start", torch.int32, 1, cache.device)
     _shape(cache_start, "cache_start", (B,))
     _err(err, cache.device)
-    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
-        st = lib().prcr_quant_append(ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL),
-                                     int(H), layer, _ptr(raw_k), _ptr(raw_v), S, _ptr(pos), _ptr(n_tokens),
-                                     _ptr(cache_start), _ptr(err), _stream(stream, cache.device))
-    _check("prcr_quant_append", st)
+    _launch("prcr_quant_append", cache.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()),
+            dtype, int(B), int(NL), int(H), layer, _ptr(raw_k), _ptr(raw_v), S, _ptr(pos), _ptr(n_tokens),
+            _ptr(cache_start), _ptr(err))
 
 
 def quant_rebind_inject(rope: Rope, mem: Memory, sel_off, sel_idx, new_pos, cache: QuantCache, cache_len,
@@ -986,12 +967,9 @@ def quant_rebind_inject(rope: Rope, mem: Memory, sel_off, sel_idx, new_pos, cach
     _shape(new_cache_len, "new_cache_len", (B,))
     _shape(slot_mapping, "slot_mapping", (total_k,))
     _err(err, mem.device)
-    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
-        st = lib().prcr_quant_rebind_inject(
-            ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()), _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(new_pos),
-            ctypes.byref(cache.to_c()), _ptr(cache_len), _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err),
-            _stream(stream, mem.device))
-    _check("prcr_quant_rebind_inject", st)
+    _launch("prcr_quant_rebind_inject", mem.device, stream, ctypes.byref(rope.to_c()), ctypes.byref(mem.to_c()),
+            _ptr(sel_off), _ptr(sel_idx), total_k, _ptr(new_pos), ctypes.byref(cache.to_c()), _ptr(cache_len),
+            _ptr(new_cache_len), _ptr(slot_mapping), _ptr(err))
     return new_cache_len, slot_mapping
 
 
@@ -1020,10 +998,8 @@ def quant_read(cache: QuantCache, layer: int, cache_len, dtype, k=None, v=None, 
     _shape(k, "k", shape)
     _shape(v, "v", shape)
     _err(err, cache.device)
-    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
-        st = lib().prcr_quant_read(ctypes.byref(cache.to_c()), _dtype_code(k), int(B), int(NL), int(H), int(D), layer,
-                                   _ptr(cache_len), _ptr(k), _ptr(v), S, _ptr(err), _stream(stream, cache.device))
-    _check("prcr_quant_read", st)
+    _launch("prcr_quant_read", cache.device, stream, ctypes.byref(cache.to_c()), _dtype_code(k), int(B),
+            int(NL), int(H), int(D), layer, _ptr(cache_len), _ptr(k), _ptr(v), S, _ptr(err))
     return k, v
 
 
@@ -1062,10 +1038,7 @@ def quant_decode_attention(rope: Rope, cache: QuantCache, layer: int, q, q_pos, 
     workspace = _workspace(workspace, quant_decode_workspace_bytes(cache, Hq), cache.device, stream)
     _err(err, cache.device)
     sc = float(D) ** -0.5 if scale is None else float(scale)
-    with torch.cuda.device(cache.device):   # (the default stream is the current device's)
-        st = lib().prcr_quant_decode_attention(
-            ctypes.byref(rope.to_c()), ctypes.byref(cache.to_c()), dtype, int(B), int(NL), int(H), layer, _ptr(q), int(Hq),
-            _ptr(q_pos), _ptr(cache_len), sc, _ptr(out), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _ptr(err), _stream(stream, cache.device))
-    _check("prcr_quant_decode_attention", st)
+    _launch("prcr_quant_decode_attention", cache.device, stream, ctypes.byref(rope.to_c()),
+            ctypes.byref(cache.to_c()), dtype, int(B), int(NL), int(H), layer, _ptr(q), int(Hq), _ptr(q_pos),
+            _ptr(cache_len), sc, _ptr(out), _ptr(workspace), workspace.nbytes, _ptr(err))
     return out

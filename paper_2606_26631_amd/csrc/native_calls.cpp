@@ -163,10 +163,12 @@ hipStream_t handle_of(PyObject *number) {
 // current one that memory is the other stream's: one of the current stream's blocks might
 // still be read there when the kernels write it, and would be handed out again, once the
 // call has dropped it, while they run.  What the caller is given is used on the current
-// stream, so it is recorded there and is not handed out again before that use.
+// stream, so it is recorded there and is not handed out again before that use.  The tensors'
+// device is the current one meanwhile: torch's default stream has no number of its own, and
+// stands for the current device's.
 class Launch {
  public:
-  Launch(PyObject *stream, at::Device device) : device_(device) {
+  Launch(PyObject *stream, at::Device device) : device_(device), on_device_(device) {
     const Ref index(PyLong_FromLong(device.index()));
     handle_ = handle_of(PyObject_CallOneArg(g_raw_stream, index.get()));
     if (stream == Py_None) return;
@@ -194,6 +196,7 @@ class Launch {
 
  private:
   at::Device device_;
+  c10::DeviceGuard on_device_;
   hipStream_t handle_;
   bool other_ = false;
   std::optional<c10::Stream> on_;
@@ -768,7 +771,6 @@ PyObject *quant_append(Args a) {
   prcr_status st;
   {
     Unlocked u;
-    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     st = prcr_quant_append(&rope, &cache.c, dtype, cache.batch, cache.n_layers, cache.n_kv_heads, layer, ptr<void>(raw_k),
                            ptr<void>(raw_v), s_src, ptr<int32_t>(pos), ptr<int32_t>(n_tokens), ptr<int32_t>(start),
                            ptr<int32_t>(err), on.handle());
@@ -795,7 +797,6 @@ PyObject *quant_rebind_inject(Args a) {
   prcr_status st;
   {
     Unlocked u;
-    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     new_len.make(on);
     slots.make(on);
     st = prcr_quant_rebind_inject(&rope, &m.c, ptr<int32_t>(sel.off), ptr<int32_t>(sel.idx), sel.k, ptr<double>(new_pos),
@@ -824,7 +825,6 @@ PyObject *quant_read(Args a) {
   prcr_status st;
   {
     Unlocked u;
-    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     k.make(on);
     v.make(on);
     st = prcr_quant_read(&cache.c, dtype_of(k.t), cache.batch, cache.n_layers, cache.n_kv_heads, cache.head_dim, layer,
@@ -858,7 +858,6 @@ PyObject *quant_decode_attention(Args a) {
   prcr_status st;
   {
     Unlocked u;
-    const c10::DeviceGuard on_device(cache.device);   // (the default stream is the current device's)
     out.make(on);
     ws.make(on);
     st = prcr_quant_decode_attention(&rope, &cache.c, dtype, cache.batch, cache.n_layers, cache.n_kv_heads, layer,
