@@ -365,6 +365,8 @@ class Cache:
 
     def check_matches(self, mem: Memory):
         B, M, NL, H, D = mem.k.shape
+        if self.device != mem.device:
+            raise ValueError(f"cache is on {self.device}, expected {mem.device}")
         if self.k.dtype != mem.k.dtype:
             raise ValueError("cache and memory element types differ")
         if self.paged:

@@ -272,7 +272,7 @@ struct Store {
   int64_t n_kv_heads() const { return k.size(paged ? 3 : 2); }
   int64_t rows() const { return paged ? table.size(0) : k.size(0); }   // sequences
   void check_matches(const Mem &m) const {
-    if (k.scalar_type() != m.k.scalar_type() || rows() != m.c.batch || n_layers() != m.c.n_layers ||
+    if (device != m.device || k.scalar_type() != m.k.scalar_type() || rows() != m.c.batch || n_layers() != m.c.n_layers ||
         n_kv_heads() != m.c.n_kv_heads || k.size(4) != m.c.head_dim)
       throw Skip();
   }

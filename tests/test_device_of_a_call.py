@@ -89,3 +89,22 @@ def test_the_tensors_gpu_is_current_in_every_call(gpu):
     on_stream = {n for n in dir(prcr) if callable(getattr(prcr, n)) and not n.endswith("bytes")}
     on_stream -= {"Cache", "Memory", "Rope", "QuantCache", "PrcrError", "lib"}
     assert {f"prcr_{n}" for n in on_stream} == set(todo)
+
+
+def test_a_cache_on_another_device_than_the_memory_is_refused(gpu):
+    """(The meta device stands for another GPU.)"""
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)
+    rope, rows = prcr.Rope(D, (8, 12, 12)), torch.zeros(B, M, NL, H, D)
+    mem = prcr.Memory(rows, rows, ints(B, M, 3), ints(B))
+    far = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device="meta")
+    sel, new_pos, k = (ints(B + 1), ints(3)), torch.zeros(3, 3, dtype=torch.float64), torch.zeros(B, 4, H, D)
+    cache = prcr.Cache(far(B, NL, H, S, D), far(B, NL, H, S, D))
+    cache8 = prcr.QuantCache(*(far(B, NL, H, S, D, dtype=torch.int8) for _ in range(2)), *(far(B, NL, H, S) for _ in range(2)))
+    for call in (lambda: prcr.rebind_inject(rope, mem, *sel, new_pos, cache, ints(B)),
+                 lambda: prcr.revisit(rope, mem, *sel, ints(B), cache, ints(B)),
+                 lambda: prcr.prefill_capture(rope, mem, 0, k, k, ints(B, 4, 3), ints(B), ints(B, 4), cache, ints(B)),
+                 lambda: prcr.quant_rebind_inject(rope, mem, *sel, new_pos, cache8, ints(B)),
+                 lambda: prcr.evict(cache, ints(B), far(B, H, S), 4, mem=mem)):
+        with pytest.raises(ValueError, match="is on .*, expected"):
+            call()
+    assert not gpu.calls
