@@ -3,13 +3,14 @@
 // the token's position, as a cache of the rows' type holds it, and then it and the value row
 // are quantised: their largest magnitude, the scale, the codes.
 //
-// A wave has 8 tokens (bf16, head_dim 128; 4 or 16 else) side by side, 8 lanes to each, and goes through
-// their rows (heads, or layers and heads), so that what it stores of a row are neighbouring slots: whole lines
-// of codes, and scales next to each other.  A workgroup's waves share the tokens' angles (in double precision, in
-// LDS) and take the rows in turn; keys and values are separate workgroups.  With a lane's angles computed
-// by itself and keys and values in one wave, 8 prompts of 2,560 tokens took 29.3 us, now 25.0; 16 x 512
-// revisited tokens 158 and 144.  What bounds it is reading the rows and writing the codes (5.1 and 4.9 TB/s), of
-// few tokens the dependent loads before a row: lengths, table entry and row in two rounds (64 tokens 4.6 us).
+// A wave has its tokens side by side: 8 of 8 lanes each (bf16 rows of 128, float32 rows of 64), 16 of 4 (bf16, 64) or 4
+// of 16 (float32, 128).  It goes through their rows (heads, or layers and heads), so that what it stores of a row
+// are neighbouring slots: whole lines of codes, and scales next to each other.  A workgroup's waves share the tokens'
+// angles (in double precision, in LDS) and take the rows in turn; keys and values are separate workgroups.  With a lane's
+// angles computed by itself and keys and values in one wave, 8 prompts of 2,560 tokens took 29.3 us, now 25.0; 16 x
+// 512 revisited tokens 158 and 143.  What bounds it is reading the rows and writing the codes (5.1 and 5.0 TB/s), of
+// few tokens the dependent loads before a row: lengths, table entry and row in two rounds (64 paged tokens of
+// 4 heads 4.7 us; a launch without a token 4.4).
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -360,13 +361,27 @@ hipError_t launch(const QuantWriteParams &in, hipStream_t stream) {
   QuantWriteParams p = in;
   p.by_seq = Divisor::of(kRebind ? 1 : p.s_src);
   p.by_heads = Divisor::of(p.to.n_kv_heads);
-  // A wave with four rows spreads what it does once a token (half of a row's work) over them, and
-  // of the angles computes its share: 8 prompts of 2,560 tokens take 25.4 us with four rows and two
-  // waves to the 8 heads, 26.4 with two and four, 26.7 with all eight and one; 64 of 4 heads 16.5 with
-  // four, 17.0 with two rows and 20.7 with one.  Few rows are the latency of one wave, shortest with the most
-  // waves: 64 tokens of 4 heads 5.5 and 7.1 us.  A revisit's many rows are dealt to four waves, as many to each
-  // as leave a thousand waves an array, up to 28 (float32: 4): 4 x 64 tokens of 112 rows take 9.2 us with 4,
-  // 11.6 with 8, 24.8 with 28, and 16 x 512 tokens 145 us with 28, 142 with 8, 158 with 4.
+  // Waves that share a group of tokens spread over them what is done once a token (half of a row's work), and of
+  // the angles compute their share.  Few rows are the latency of one wave, shortest with the most waves; of many, a
+  // wave has four.  Kernel times in us, bf16 rows of 128, one, two and four waves to a group, of 4 and of 8 heads:
+  //       64 tokens    6.8   5.2   4.5      9.9   6.7   5.2
+  //    2,000           8.1   6.1   5.0     12.0   8.2   6.0
+  //    4,000           8.7   6.7   6.5     12.7   9.4   8.0
+  //    8,000           9.6   8.6   9.7     14.7  12.9  14.5
+  //   20,480          17.0  16.2  19.7     29.0  27.2  28.5
+  // From 2,048 units on the rule gives 4 heads one wave and 8 heads two, where up to some 5,000 tokens twice as many
+  // are faster: six ragged turns, 4,186 tokens in 6,558 rows, 4 heads, take 9.1 us so, 7.9 with two, 8.4 with four.
+  // (That is not the padding: without it they take 8.7, and as many rows without a token 4.5.)
+  //
+  // A revisit's many rows are dealt to four waves, as many to each as leave a thousand waves an array, up to 28
+  // (float32: 4).  4 x 64 tokens of 28 x 4 rows, with 2, 4, 8 and 28 a wave: 10.6, 8.2, 11.5 and 24.3 us, 4 x 256
+  // tokens 29, 23.2, 20.5 and 27.8 (the rule: 4 and 14).  16 x 512 tokens, bf16 rows of 128, up to 4, 8, 16 and 28 a wave:
+  //   28 x 4    149  138  132  128   (memories of 2,304 tokens and long caches, paged: 152, 139, 137, 137)
+  //   36 x 8    366  337  339  343
+  //   64 x 8    655  605  616  624
+  //   13 x 5     98   89   86   80
+  // and 32 x 64 tokens of 28 x 4 rows 41.6, 38.3, 39.0 and 39.1, paged 42.2, 38.8, 38.3 and 37.2.  float32, paged, up
+  // to 4, 8 and 28: 28 x 4 rows 228, 231 and 242, 36 x 8 549, 570 and 590, 13 x 5 140, 143 and 145.
   constexpr int kGroup = kWave / (D / 2 / Store<T>::kPerChunk);
   const int64_t units = (static_cast<int64_t>(p.n_tok) + kGroup - 1) / kGroup * p.rows;   // a group of tokens' row
   if constexpr (kRebind) {
